@@ -298,7 +298,8 @@ oz_status_t oz_reconstruct(int64_t m, int64_t n, const void *R, int64_t ldr,
                            void *stream);
 
 /* Synchronises `stream`, then returns and clears the device status of the current device: the first
- * that applies of OZ_ERR_CUDA, OZ_ERR_TIMEOUT, OZ_ERR_NONFINITE_INPUT, OZ_ERR_RANGE, else OZ_OK.
+ * that applies of OZ_ERR_CUDA, OZ_ERR_TIMEOUT, OZ_ERR_INVALID_ARG (offsets of a grouped product), OZ_ERR_NONFINITE_INPUT,
+ * OZ_ERR_RANGE, else OZ_OK.
  *
  * OZ_ERR_RANGE is the exponent-span check (Algorithm 1, last line: "ESC check"; the paper leaves the
  * criterion to its sources, this is the library's reading).  With the norm-based scale rule
@@ -315,6 +316,53 @@ oz_status_t oz_query_status(void *stream);
 /* Synchronises `stream`, stores in *rows (host) the number of rows that calls with OZ_FALLBACK_FP64
  * re-issued on the native FP64 path on the current device since the last such query, and clears it. */
 oz_status_t oz_query_fallback_rows(void *stream, int64_t *rows);
+
+/* ------------------------------------------------------------------------------------------
+ * Products of 16-bit matrices: the layers of experts of a language model
+ *
+ * Types of the entry points below: bfloat16 and IEEE half precision operands, FP32 accumulation, results
+ * in the operands' type (rounded once) or in FP32.  Conventions as above (column-major, device pointers
+ * aligned to their element type, nothing enqueued after a host-detectable error, internal work on `stream`
+ * only), with these differences: no workspace registered with oz_set_workspace() is used, Inf and NaN go
+ * through the arithmetic like in any FP32 product and set no status, and the exponent-span check does not apply.
+ * A row-major matrix is the column-major transpose: a (tokens, features) array of a framework is
+ * a features x tokens matrix here, one column a token. */
+typedef enum { OZ_BF16 = 0, OZ_F16 = 1, OZ_F32 = 2 } oz_type_t;
+
+#define OZ_GROUPS_MAX 2048
+#define OZ_EXTENT_MAX 1073741824      /* largest m, n, k of these entry points */
+
+/* Products grouped by ragged numbers of columns (the tokens of each expert):
+ *     C(:, j) = beta C(:, j) + op(A_g) B(:, j)     for offsets[g] <= j < offsets[g + 1],  g = 0 .. groups - 1
+ * op(A_g) is m x k: A_g = A + g strideA itself, column-major with lda >= m (transA = 0), or the transpose of the k x m
+ * matrix there, lda >= k (transA = 1); strideA >= 0 in elements, 0 for one matrix that all groups share.  B is k x n, C m x n.
+ * The forward pass of a layer whose weights are (groups, m, k) row-major is transA = 1, the gradient of its inputs
+ * transA = 0 of the same array with m and k exchanged.
+ * offsets: groups + 1 DEVICE int64, non-decreasing, 0 <= offsets[0], offsets[groups] <= n; groups may be
+ * empty.  Columns of C that belong to no group keep what they hold; columns of B that belong to none are not used.
+ * They are read when the kernel runs.  Offsets that decrease or leave [0, n] make no access out of range, but leave
+ * columns of C undefined, and oz_query_status() returns OZ_ERR_INVALID_ARG.
+ * beta is 0 (C is not read) or 1; k = 0 gives C = 0 on the columns of the groups, or C unchanged for beta = 1.
+ * ctype: `type` or OZ_F32.  C must not overlap the operands.
+ * The tensor cores are fed by bulk copies, which want A and B 16-byte aligned and lda, ldb, strideA multiples of 8;
+ * operands that are not take a kernel without tensor cores, far slower.
+ * OZ_ERR_UNSUPPORTED: another beta, more than OZ_GROUPS_MAX groups, an extent above OZ_EXTENT_MAX. */
+oz_status_t oz_gemm_grouped(int transA, int64_t m, int64_t n, int64_t k, int64_t groups, const int64_t *offsets,
+                            oz_type_t type, const void *A, int64_t lda, int64_t strideA, const void *B,
+                            int64_t ldb, oz_type_t ctype, double beta, void *C, int64_t ldc, void *stream);
+
+/* Products grouped by ragged ranges of the inner dimension (the gradient of each expert's weights):
+ *     C_g = beta C_g + sum over offsets[g] <= t < offsets[g + 1] of A(:, t) B(:, t)^T
+ * A is m x tokens (lda >= m), B n x tokens (ldb >= n), C_g = C + g strideC is m x n (ldc >= m; with several groups
+ * strideC >= ldc (n - 1) + m).  An empty group's C_g becomes zero, or stays for beta = 1.  Columns of A and B that belong to no
+ * group are not used, whatever they hold.  Offsets, types, alignment and errors as for oz_gemm_grouped(); what decreasing offsets
+ * leave undefined is all of C.
+ * The gradient of (groups, m, k) row-major weights from inputs x (tokens, k) and output gradients dy (tokens, m)
+ * is A = x, B = dy. */
+oz_status_t oz_gemm_grouped_wgrad(int64_t m, int64_t n, int64_t tokens, int64_t groups, const int64_t *offsets,
+                                  oz_type_t type, const void *A, int64_t lda, const void *B, int64_t ldb,
+                                  oz_type_t ctype, double beta, void *C, int64_t ldc, int64_t strideC,
+                                  void *stream);
 
 /* Optional per-stage timing hook for benchmarks (the paper's Algorithm 1 prices each stage
  * separately), kept per device: it applies to the device that is current when it is set.  `events`

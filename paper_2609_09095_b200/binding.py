@@ -27,18 +27,21 @@ OZ_STORAGE_FUSED = 0x10000
 OZ_K_MAX = 1048576
 OZ_NONFINITE_SHIFT = -(2 ** 31)
 OZ_STATIC_MAX_LINES = 262144
+OZ_BF16, OZ_F16, OZ_F32 = 0, 1, 2
+OZ_GROUPS_MAX = 2048
+OZ_EXTENT_MAX = 1073741824
 
 EXPORTS = ["oz_set_info", "oz_plane_count", "oz_plane_count_side", "oz_row_pitch", "oz_residue_elem_bytes", "oz_workspace_bytes", "oz_set_workspace", "oz_dgemm",
            "oz_dgemm_ex", "oz_dgemm_host", "oz_operand_bytes", "oz_product_workspace_bytes", "oz_prepare_operand",
            "oz_dgemm_prepared", "oz_deconstruct", "oz_deconstruct_static",
-           "oz_residue_gemm", "oz_reconstruct",
+           "oz_residue_gemm", "oz_reconstruct", "oz_gemm_grouped", "oz_gemm_grouped_wgrad",
            "oz_query_status", "oz_query_fallback_rows", "oz_set_stage_events", "oz_launch_count", "oz_status_string"]
 
 __all__ = EXPORTS + ["EXPORTS", "OzError", "load", "check", "LIB_PATH", "OZ_OK", "OZ_ERR_INVALID_ARG",
                      "OZ_ERR_UNSUPPORTED", "OZ_ERR_WORKSPACE", "OZ_ERR_CUDA",
                      "OZ_ERR_NONFINITE_INPUT", "OZ_ERR_RANGE", "OZ_ERR_TIMEOUT", "OZ_SET_S",
                      "OZ_SET_E", "OZ_SET_A", "OZ_SUB_FP8", "OZ_SUB_INT8", "OZ_SUB_INT8_NATIVE", "OZ_QUANT_RN", "OZ_QUANT_TZ",
-                     "OZ_SCALE_MAXEXP", "OZ_SCALE_CS", "OZ_SCALE_ACCURATE", "OZ_ACC_MERGED", "OZ_ACC_SEPARATE", "OZ_RECON_TENSOR", "OZ_FALLBACK_FP64", "OZ_STORAGE_FUSED", "OZ_K_MAX", "OZ_NONFINITE_SHIFT", "OZ_STATIC_MAX_LINES"]
+                     "OZ_SCALE_MAXEXP", "OZ_SCALE_CS", "OZ_SCALE_ACCURATE", "OZ_ACC_MERGED", "OZ_ACC_SEPARATE", "OZ_RECON_TENSOR", "OZ_FALLBACK_FP64", "OZ_STORAGE_FUSED", "OZ_K_MAX", "OZ_NONFINITE_SHIFT", "OZ_STATIC_MAX_LINES", "OZ_BF16", "OZ_F16", "OZ_F32", "OZ_GROUPS_MAX", "OZ_EXTENT_MAX"]
 
 _lib = None
 
@@ -83,6 +86,8 @@ def load() -> C.CDLL:
     lib.oz_residue_gemm.argtypes = [i64, i64, i64, vp, i64, i64, vp, i64, i64, i32, u32, vp, i64,
                                     i64, vp]
     lib.oz_reconstruct.argtypes = [i64, i64, vp, i64, i64, vp, vp, i32, dbl, dbl, vp, i64, vp]
+    lib.oz_gemm_grouped.argtypes = [i32, i64, i64, i64, i64, vp, i32, vp, i64, i64, vp, i64, i32, dbl, vp, i64, vp]
+    lib.oz_gemm_grouped_wgrad.argtypes = [i64, i64, i64, i64, vp, i32, vp, i64, vp, i64, i32, dbl, vp, i64, i64, vp]
     lib.oz_query_status.argtypes = [vp]
     lib.oz_query_fallback_rows.argtypes = [vp, C.POINTER(C.c_int64)]
     lib.oz_set_stage_events.argtypes = [C.POINTER(vp)]
@@ -219,6 +224,16 @@ def oz_reconstruct(m, n, R, ldr, mod_stride, shiftA, shiftB, modset, alpha, beta
                    stream=None) -> int:
     return load().oz_reconstruct(m, n, _ptr(R), ldr, mod_stride, _ptr(shiftA), _ptr(shiftB), modset,
                                  alpha, beta, _ptr(Cm), ldc, _stream(stream))
+
+
+def oz_gemm_grouped(transA, m, n, k, groups, offsets, dtype, A, lda, strideA, B, ldb, ctype, beta, Cm, ldc, stream=None) -> int:
+    return load().oz_gemm_grouped(transA, m, n, k, groups, _ptr(offsets), dtype, _ptr(A), lda, strideA, _ptr(B), ldb, ctype, beta,
+                                  _ptr(Cm), ldc, _stream(stream))
+
+
+def oz_gemm_grouped_wgrad(m, n, tokens, groups, offsets, dtype, A, lda, B, ldb, ctype, beta, Cm, ldc, strideC, stream=None) -> int:
+    return load().oz_gemm_grouped_wgrad(m, n, tokens, groups, _ptr(offsets), dtype, _ptr(A), lda, _ptr(B), ldb, ctype, beta,
+                                        _ptr(Cm), ldc, strideC, _stream(stream))
 
 
 def oz_query_status(stream=None) -> int:

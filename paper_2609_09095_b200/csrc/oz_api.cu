@@ -1022,6 +1022,7 @@ oz_status_t oz_query_status(void *stream)
     OZ_CUDA_CHECK(cudaMemcpyToSymbol(g_status, kStatusReset, sizeof(word)));   // word 4 has its own query
     if (cudaGetLastError() != cudaSuccess) return OZ_ERR_CUDA;
     if (word[0] & (1u << OZ_ERR_TIMEOUT)) return OZ_ERR_TIMEOUT;
+    if (word[0] & (1u << OZ_ERR_INVALID_ARG)) return OZ_ERR_INVALID_ARG;
     if (word[0] & (1u << OZ_ERR_NONFINITE_INPUT)) return OZ_ERR_NONFINITE_INPUT;
     // exponent-span check: an operand that was not scanned since the last query counts as flat
     const uint64_t qa = word[1] > 65536u ? 65536u : word[1], qb = word[2] > 65536u ? 65536u : word[2];

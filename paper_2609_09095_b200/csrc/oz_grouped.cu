@@ -1,0 +1,289 @@
+// Products of 16-bit matrices grouped by ragged sizes (oz_gemm_grouped, oz_gemm_grouped_wgrad): the forward pass of a layer
+// of experts and the gradients of its inputs and weights.
+//
+//   columns grouped:  C(:, j) = beta C(:, j) + op(A_g) B(:, j)                         for the columns j of group g
+//   inner grouped:    C_g     = beta C_g + sum over the columns t of group g of A(:, t) B(:, t)^T
+//
+// The groups' offsets are on the device, written by whatever sorts the tokens, so that the tiles of a launch are counted on the
+// device too: every block reads the offsets, counts the tiles of each group and walks the list of all tiles.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <atomic>
+
+#include "oz_internal.h"
+
+namespace oz {
+namespace {
+
+constexpr int64_t kMaxGroups = OZ_GROUPS_MAX;
+
+struct GroupedParams {
+    int64_t m, n, k;                // columns grouped: C is m x n, k the inner dimension; inner grouped: every C_g is m x n
+    int64_t columns;                // what the offsets divide: n, or the columns of A and B
+    int groups;
+    const int64_t *offsets;
+    const void *A, *B;
+    // element (i, kk) of op(A_g) at g strideA + i rowA + kk innerA, element (kk, j) of B at kk innerB + j colB
+    int64_t strideA, rowA, innerA, innerB, colB;
+    void *C;
+    int64_t ldc, strideC;
+    int ctype, accumulate;
+    unsigned int *status;
+};
+
+// Where the groups begin and end, in shared memory: cuts[g] .. cuts[g + 1], and, for the form with grouped columns, how many tiles
+// of `width` columns lie before each group.  All threads of the block take part.  The cuts are the offsets held to [0, columns] and to
+// the largest before them: offsets out of order or range are reported, and what comes of them indexes nothing out of range.
+__device__ void read_groups(const GroupedParams &p, int width, int *cuts, int *before)
+{
+    for (int g = threadIdx.x; g <= p.groups; g += blockDim.x) {
+        const int64_t o = p.offsets[g];
+        const int64_t held = o < 0 ? 0 : (o > p.columns ? p.columns : o);
+        if (held != o || (g > 0 && p.offsets[g - 1] > o)) atomicOr(p.status, 1u << OZ_ERR_INVALID_ARG);
+        cuts[g] = static_cast<int>(held);
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        int start = cuts[0], sum = 0;                    // end of the last group so far, tiles so far
+        for (int g0 = 0; g0 < p.groups; g0 += 32) {
+            const int g = g0 + lane;
+            int end = g < p.groups ? cuts[g + 1] : 0;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int other = __shfl_up_sync(0xFFFFFFFFu, end, d);
+                if (lane >= d) end = max(end, other);
+            }
+            end = max(end, start);
+            const int last = __shfl_up_sync(0xFFFFFFFFu, end, 1);
+            const int len = end - (lane == 0 ? start : last);
+            const int tiles = g < p.groups ? (len + width - 1) / width : 0;
+            int upto = tiles;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int other = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+                if (lane >= d) upto += other;
+            }
+            if (g < p.groups) {
+                cuts[g + 1] = end;
+                if (before) before[g] = sum + upto - tiles;
+            }
+            sum += __shfl_sync(0xFFFFFFFFu, upto, 31);
+            start = __shfl_sync(0xFFFFFFFFu, end, 31);
+        }
+        if (lane == 0 && before) before[p.groups] = sum;
+    }
+    __syncthreads();
+}
+
+// the group that tile `t` of all tiles belongs to: the last g with before[g] <= t (t < before[groups])
+__device__ __forceinline__ int group_of(const int *before, int groups, int t)
+{
+    int lo = 0, hi = groups;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (before[mid] <= t) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <class T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
+// C[at] = v, or the rounded sum with what is there (one rounding either way)
+__device__ __forceinline__ void store_result(void *C, int64_t at, float v, int ctype, int accumulate)
+{
+    if (ctype == OZ_F32) {
+        float *c = static_cast<float *>(C) + at;
+        *c = accumulate ? *c + v : v;
+    } else if (ctype == OZ_BF16) {
+        __nv_bfloat16 *c = static_cast<__nv_bfloat16 *>(C) + at;
+        *c = __float2bfloat16_rn(accumulate ? __bfloat162float(*c) + v : v);
+    } else {
+        __half *c = static_cast<__half *>(C) + at;
+        *c = __float2half_rn(accumulate ? __half2float(*c) + v : v);
+    }
+}
+
+// ---------------------------------------------------------------- any alignment, without tensor cores
+// A block computes tiles of 64 x 64 of C, 4 x 4 a thread, from pieces of 16 inner indices in shared memory; every operand element
+// is fetched by itself, so that any leading dimension and address will do.  Bound: the FP32 pipe.
+constexpr int PLAIN_TILE = 64, PLAIN_K = 16, PLAIN_THREADS = 256;
+
+template <class T, bool INNER>
+__global__ void __launch_bounds__(PLAIN_THREADS) grouped_plain_kernel(const GroupedParams p)
+{
+    extern __shared__ int table[];
+    __shared__ float sa[PLAIN_K][PLAIN_TILE + 4], sb[PLAIN_K][PLAIN_TILE + 4];
+    dependency_release();
+    dependency_wait();
+    int *cuts = table, *before = INNER ? nullptr : table + p.groups + 1;
+    read_groups(p, PLAIN_TILE, cuts, before);
+    const T *A = static_cast<const T *>(p.A), *B = static_cast<const T *>(p.B);
+    const int64_t tiles_m = (p.m + PLAIN_TILE - 1) / PLAIN_TILE, tiles_n = (p.n + PLAIN_TILE - 1) / PLAIN_TILE;
+    const int64_t total = INNER ? p.groups * tiles_m * tiles_n : before[p.groups] * tiles_m;
+    const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
+        int g;
+        int64_t i0, j0, j1, k0, k1;
+        if (INNER) {
+            g = static_cast<int>(item / (tiles_m * tiles_n));
+            const int64_t t = item % (tiles_m * tiles_n);
+            i0 = t % tiles_m * PLAIN_TILE;
+            j0 = t / tiles_m * PLAIN_TILE;
+            j1 = p.n;
+            k0 = cuts[g];
+            k1 = cuts[g + 1];
+        } else {
+            const int t = static_cast<int>(item / tiles_m);
+            g = group_of(before, p.groups, t);
+            i0 = item % tiles_m * PLAIN_TILE;
+            j0 = cuts[g] + static_cast<int64_t>(t - before[g]) * PLAIN_TILE;
+            j1 = cuts[g + 1];
+            k0 = 0;
+            k1 = p.k;
+        }
+        float acc[4][4] = {};
+        for (int64_t kk0 = k0; kk0 < k1; kk0 += PLAIN_K) {
+            // consecutive threads along the direction in which the elements lie one behind the other
+#pragma unroll
+            for (int e = threadIdx.x; e < PLAIN_K * PLAIN_TILE; e += PLAIN_THREADS) {
+                const int ka = p.rowA == 1 ? e / PLAIN_TILE : e % PLAIN_K, ia = p.rowA == 1 ? e % PLAIN_TILE : e / PLAIN_K;
+                const int kb = p.colB == 1 ? e / PLAIN_TILE : e % PLAIN_K, jb = p.colB == 1 ? e % PLAIN_TILE : e / PLAIN_K;
+                sa[ka][ia] = kk0 + ka < k1 && i0 + ia < p.m
+                                 ? to_float(A[g * p.strideA + (i0 + ia) * p.rowA + (kk0 + ka) * p.innerA]) : 0.0f;
+                sb[kb][jb] = kk0 + kb < k1 && j0 + jb < j1 ? to_float(B[(kk0 + kb) * p.innerB + (j0 + jb) * p.colB]) : 0.0f;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int kk = 0; kk < PLAIN_K; ++kk) {
+                const float4 a = *reinterpret_cast<const float4 *>(&sa[kk][4 * tx]), b = *reinterpret_cast<const float4 *>(&sb[kk][4 * ty]);
+                const float av[4] = {a.x, a.y, a.z, a.w}, bv[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(av[i], bv[j], acc[i][j]);
+            }
+            __syncthreads();
+        }
+        if (k1 <= k0 && p.accumulate) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t row = i0 + 4 * tx + i, col = j0 + 4 * ty + j;
+                if (row < p.m && col < j1)
+                    store_result(p.C, (INNER ? g * p.strideC : 0) + row + col * p.ldc, acc[i][j], p.ctype, p.accumulate);
+            }
+    }
+}
+
+template <class T, bool INNER>
+oz_status_t launch_plain(const GroupedParams &p, cudaStream_t stream)
+{
+    // enough blocks for the tiles of grouped columns that the host can count on, four of them a multiprocessor at most
+    const int64_t tiles_m = (p.m + PLAIN_TILE - 1) / PLAIN_TILE, tiles_n = (p.n + PLAIN_TILE - 1) / PLAIN_TILE;
+    const int64_t most = INNER ? p.groups * tiles_m * tiles_n : tiles_m * (tiles_n + p.groups);
+    const int64_t grid = most < 4 * sm_count() ? most : 4 * sm_count();
+    OZ_CUDA_CHECK(launch(grouped_plain_kernel<T, INNER>, dim3(static_cast<unsigned>(grid)), PLAIN_THREADS,
+                         2 * (p.groups + 1) * sizeof(int), stream, p));
+    count_launch();
+    return OZ_OK;
+}
+
+// ---------------------------------------------------------------- checks that both entry points share
+bool aligned_to(const void *ptr, size_t bytes) { return reinterpret_cast<uintptr_t>(ptr) % bytes == 0; }
+
+size_t size_of_type(int type) { return type == OZ_F32 ? 4 : 2; }
+
+oz_status_t check_types(oz_type_t type, oz_type_t ctype, double beta, const void *A, const void *B, const void *C)
+{
+    if ((type != OZ_BF16 && type != OZ_F16) || (ctype != type && ctype != OZ_F32)) return OZ_ERR_INVALID_ARG;
+    if (!aligned_to(A, 2) || !aligned_to(B, 2) || !aligned_to(C, size_of_type(ctype))) return OZ_ERR_INVALID_ARG;
+    return beta == 0.0 || beta == 1.0 ? OZ_OK : OZ_ERR_UNSUPPORTED;
+}
+
+template <bool INNER>
+oz_status_t launch_grouped(GroupedParams &p, oz_type_t type, cudaStream_t stream)
+{
+    oz_status_t st = ensure_device_ready();
+    if (st != OZ_OK) return st;
+    p.status = device_status_word();
+    return type == OZ_BF16 ? launch_plain<__nv_bfloat16, INNER>(p, stream) : launch_plain<__half, INNER>(p, stream);
+}
+
+}  // namespace
+}  // namespace oz
+
+using namespace oz;
+
+extern "C" {
+
+oz_status_t oz_gemm_grouped(int transA, int64_t m, int64_t n, int64_t k, int64_t groups, const int64_t *offsets,
+                            oz_type_t type, const void *A, int64_t lda, int64_t strideA, const void *B, int64_t ldb,
+                            oz_type_t ctype, double beta, void *C, int64_t ldc, void *stream)
+{
+    if (m < 0 || n < 0 || k < 0 || groups < 0 || strideA < 0 || (transA != 0 && transA != 1)) return OZ_ERR_INVALID_ARG;
+    oz_status_t st = check_types(type, ctype, beta, A, B, C);
+    if (st != OZ_OK) return st;
+    if (m > OZ_EXTENT_MAX || n > OZ_EXTENT_MAX || k > OZ_EXTENT_MAX || groups > kMaxGroups) return OZ_ERR_UNSUPPORTED;
+    if (m == 0 || n == 0 || groups == 0) return OZ_OK;
+    if (!offsets || !aligned_to(offsets, 8) || !C || ldc < m) return OZ_ERR_INVALID_ARG;
+    if (k > 0 && (!A || !B || lda < (transA ? k : m) || ldb < k)) return OZ_ERR_INVALID_ARG;
+    if (k == 0 && beta == 1.0) return OZ_OK;
+    GroupedParams p{};
+    p.m = m;
+    p.n = p.columns = n;
+    p.k = k;
+    p.groups = static_cast<int>(groups);
+    p.offsets = offsets;
+    p.A = A;
+    p.B = B;
+    p.strideA = strideA;
+    p.rowA = transA ? lda : 1;
+    p.innerA = transA ? 1 : lda;
+    p.innerB = 1;
+    p.colB = ldb;
+    p.C = C;
+    p.ldc = ldc;
+    p.ctype = ctype;
+    p.accumulate = beta == 1.0;
+    return launch_grouped<false>(p, type, static_cast<cudaStream_t>(stream));
+}
+
+oz_status_t oz_gemm_grouped_wgrad(int64_t m, int64_t n, int64_t tokens, int64_t groups, const int64_t *offsets,
+                                  oz_type_t type, const void *A, int64_t lda, const void *B, int64_t ldb, oz_type_t ctype,
+                                  double beta, void *C, int64_t ldc, int64_t strideC, void *stream)
+{
+    if (m < 0 || n < 0 || tokens < 0 || groups < 0) return OZ_ERR_INVALID_ARG;
+    oz_status_t st = check_types(type, ctype, beta, A, B, C);
+    if (st != OZ_OK) return st;
+    if (m > OZ_EXTENT_MAX || n > OZ_EXTENT_MAX || tokens > OZ_EXTENT_MAX || groups > kMaxGroups) return OZ_ERR_UNSUPPORTED;
+    if (m == 0 || n == 0 || groups == 0) return OZ_OK;
+    if (!offsets || !aligned_to(offsets, 8) || !C || ldc < m) return OZ_ERR_INVALID_ARG;
+    if (groups > 1 && (strideC < m || (strideC - m) / ldc < n - 1)) return OZ_ERR_INVALID_ARG;
+    if (tokens > 0 && (!A || !B || lda < m || ldb < n)) return OZ_ERR_INVALID_ARG;
+    GroupedParams p{};
+    p.m = m;
+    p.n = n;
+    p.columns = tokens;
+    p.groups = static_cast<int>(groups);
+    p.offsets = offsets;
+    p.A = A;
+    p.B = B;
+    p.rowA = 1;
+    p.innerA = lda;
+    p.innerB = ldb;
+    p.colB = 1;
+    p.C = C;
+    p.ldc = ldc;
+    p.strideC = strideC;
+    p.ctype = ctype;
+    p.accumulate = beta == 1.0;
+    return launch_grouped<true>(p, type, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
