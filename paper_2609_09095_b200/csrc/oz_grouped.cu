@@ -11,7 +11,7 @@
 
 #include <atomic>
 
-#include "oz_internal.h"
+#include "oz_product16.cuh"
 
 namespace oz {
 namespace {
@@ -29,7 +29,9 @@ struct GroupedParams {
     void *C;
     int64_t ldc, strideC;
     int ctype, accumulate;
+    int shared_a;                   // one A for all groups
     unsigned int *status;
+    Core16 core;
 };
 
 // Where the groups begin and end, in shared memory: cuts[g] .. cuts[g + 1], and, for the form with grouped columns, how many tiles
@@ -194,6 +196,138 @@ oz_status_t launch_plain(const GroupedParams &p, cudaStream_t stream)
     return OZ_OK;
 }
 
+// ---------------------------------------------------------------- tensor cores
+// Rows of a tile are rows of C (features, whatever the group's size), its columns are those of a group (tokens) or of C_g: a group of
+// few tokens then takes an MMA of few columns, and consecutive lanes hold consecutive elements of the column-major result.
+// A group's columns are cut into equal tiles of at most BN.  The tiles that share rows of A follow one another, so that A comes from memory once.
+template <bool INNER>
+struct GroupedPolicy {
+    using Params = GroupedParams;
+    struct Tile : Tile16 {
+        int rows, valid;            // rows of C from the tile's first on, columns that belong to the group
+        int64_t c;                  // element of C at the tile's first row and column
+    };
+    static constexpr bool RAGGED_K = INNER;
+
+    static __device__ __forceinline__ void setup(const Params &p, int width, int *table)
+    {
+        read_groups(p, width, table, INNER ? nullptr : table + p.groups + 1);
+    }
+
+    template <int CG, int BN>
+    static __device__ __forceinline__ int64_t total(const Params &p, const int *table)
+    {
+        const uint32_t tiles_m = static_cast<uint32_t>((p.m + 128 * CG - 1) / (128 * CG));
+        if (INNER) return static_cast<int64_t>(p.groups) * tiles_m * static_cast<uint32_t>((p.n + BN - 1) / BN);
+        return static_cast<int64_t>(table[2 * p.groups + 1]) * tiles_m;
+    }
+
+    // (the host sends launches of 2^31 tiles and more elsewhere: 32-bit divisions are enough)
+    template <int CG, int BN>
+    static __device__ __forceinline__ Tile decode(const Params &p, const int *table, int64_t item64)
+    {
+        const uint32_t item = static_cast<uint32_t>(item64), tiles_m = static_cast<uint32_t>((p.m + 128 * CG - 1) / (128 * CG));
+        Tile t;
+        int g, i0, j0;
+        if (INNER) {
+            const uint32_t tiles_n = static_cast<uint32_t>((p.n + BN - 1) / BN), each = tiles_m * tiles_n;
+            g = static_cast<int>(item / each);
+            const uint32_t in = item - static_cast<uint32_t>(g) * each;
+            i0 = static_cast<int>(in / tiles_n) * 128 * CG;
+            j0 = static_cast<int>(in % tiles_n) * BN;
+            t.valid = static_cast<int>(min(static_cast<int64_t>(BN), p.n - j0));
+            t.k_begin = table[g];
+            t.k_len = table[g + 1] - table[g];
+            t.a_z = t.b_z = 0;
+            t.b_row = j0;
+            t.c = g * p.strideC + i0 + j0 * p.ldc;
+        } else {
+            const int *before = table + p.groups + 1;
+            g = group_of(before, p.groups, static_cast<int>(item / tiles_m));
+            const uint32_t in = item - static_cast<uint32_t>(before[g]) * tiles_m, tiles_n = static_cast<uint32_t>(before[g + 1] - before[g]);
+            const int len = table[g + 1] - table[g], nt = static_cast<int>(in % tiles_n);
+            const int width = ((len + static_cast<int>(tiles_n) - 1) / static_cast<int>(tiles_n) + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            i0 = static_cast<int>(in / tiles_n) * 128 * CG;
+            j0 = table[g] + nt * width;
+            t.valid = min(width, table[g + 1] - j0);
+            t.k_begin = 0;
+            t.k_len = static_cast<int>(p.k);
+            t.a_z = p.shared_a ? 0 : g;
+            t.b_z = 0;
+            t.b_row = j0;
+            t.c = i0 + j0 * p.ldc;
+        }
+        t.a_row = i0;
+        t.rows = static_cast<int>(p.m) - i0;
+        t.cols = (t.valid + 16 * CG - 1) / (16 * CG) * (16 * CG);
+        return t;
+    }
+
+    template <int CG, int BN>
+    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[BN / 4], int row, int col)
+    {
+        if (row >= t.rows || (t.k_len == 0 && p.accumulate)) return;
+        const int64_t at = t.c + row + col * p.ldc;
+#pragma unroll
+        for (int c = 0; c < BN / 4; ++c)
+            if (col + c < t.valid) store_result(p.C, at + c * p.ldc, acc[c], p.ctype, p.accumulate);
+    }
+};
+
+template <bool INNER, int CG, int BN>
+oz_status_t launch_tiles(GroupedParams &p, bool bf16, const CUtensorMap &mapA, const CUtensorMap &mapB, int64_t most, cudaStream_t stream)
+{
+    p.core.idesc = idesc16(bf16, p.core.a_mn, p.core.b_mn, CG);
+    return launch_product16<GroupedPolicy<INNER>, CG, BN, 1>(mapA, mapB, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
+}
+
+// tiles of 128 cg x bn at most: what the host knows of the groups is their number and that of all columns
+template <bool INNER>
+int64_t most_tiles(const GroupedParams &p, int cg, int bn)
+{
+    const int64_t tiles_m = (p.m + 128 * cg - 1) / (128 * cg);
+    if (INNER) return p.groups * tiles_m * ((p.n + bn - 1) / bn);
+    const int64_t full = p.n / bn, some = p.n < p.groups ? p.n : p.groups;
+    return tiles_m * (full + some);
+}
+
+// The tensor-core form, where the operands' addresses and strides allow bulk copies; *taken says whether it did
+template <bool INNER>
+oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStream_t stream)
+{
+    *taken = false;
+    const int64_t inner = INNER ? p.columns : p.k, lda = p.rowA == 1 ? p.innerA : p.rowA, ldb = p.colB == 1 ? p.innerB : p.colB;
+    if (inner == 0 || most_tiles<INNER>(p, 1, 32) >= (1ll << 31)) return OZ_OK;
+    p.shared_a = INNER || p.strideA == 0 || p.groups == 1;
+    if (reinterpret_cast<uintptr_t>(p.A) % 16 || reinterpret_cast<uintptr_t>(p.B) % 16 || lda % 8 || ldb % 8 || (!p.shared_a && p.strideA % 8))
+        return OZ_OK;
+    const bool bf16 = type == OZ_BF16;
+    p.core.a_mn = p.rowA == 1 && p.innerA != 1;
+    p.core.b_mn = INNER;
+    p.core.plane_z = 0;
+    p.core.status = p.status;
+    // sums that become 16-bit numbers need no segments
+    p.core.seg = p.ctype == OZ_F32 ? 4 : 1 << 24;
+    // Few columns a group: tiles as narrow, which leave the ring to the rows of A.
+    const int64_t mean = INNER ? p.n : p.n / p.groups;
+    const bool pairs = INNER || mean > 64;
+    const int bn = pairs ? 256 : mean > 32 ? 64 : 32;
+    CUtensorMap mapA, mapB;
+    const int64_t za = p.shared_a ? 1 : p.groups;
+    const int boxB = bn == 32 ? 32 : 64;
+    if (!(p.core.a_mn ? make_map16(&mapA, bf16, p.A, p.m, inner, lda, za, za > 1 ? p.strideA : lda, 64)
+                      : make_map16(&mapA, bf16, p.A, inner, p.m, lda, za, za > 1 ? p.strideA : lda, 64)) ||
+        !(INNER ? make_map16(&mapB, bf16, p.B, p.n, inner, ldb, 1, ldb, boxB) : make_map16(&mapB, bf16, p.B, inner, p.n, ldb, 1, ldb, boxB)))
+        return OZ_OK;
+    *taken = true;
+    if (pairs) return launch_tiles<INNER, 2, 256>(p, bf16, mapA, mapB, most_tiles<INNER>(p, 2, 256), stream);
+    if constexpr (!INNER) {
+        if (bn == 64) return launch_tiles<INNER, 1, 64>(p, bf16, mapA, mapB, most_tiles<INNER>(p, 1, 64), stream);
+        return launch_tiles<INNER, 1, 32>(p, bf16, mapA, mapB, most_tiles<INNER>(p, 1, 32), stream);
+    }
+    return OZ_OK;
+}
+
 // ---------------------------------------------------------------- checks that both entry points share
 bool aligned_to(const void *ptr, size_t bytes) { return reinterpret_cast<uintptr_t>(ptr) % bytes == 0; }
 
@@ -212,6 +346,9 @@ oz_status_t launch_grouped(GroupedParams &p, oz_type_t type, cudaStream_t stream
     oz_status_t st = ensure_device_ready();
     if (st != OZ_OK) return st;
     p.status = device_status_word();
+    bool taken = false;
+    st = launch_tensor<INNER>(p, type, &taken, stream);
+    if (taken || st != OZ_OK) return st;
     return type == OZ_BF16 ? launch_plain<__nv_bfloat16, INNER>(p, stream) : launch_plain<__half, INNER>(p, stream);
 }
 

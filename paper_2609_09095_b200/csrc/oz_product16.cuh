@@ -1,0 +1,403 @@
+// The core of the products of 16-bit matrices: tiles of D = A B on the 5th-generation tensor cores (kind::f16, FP32 accumulation in
+// tensor memory), for operands stored along either direction.  What a tile is, how many there are and where its result goes is a
+// policy's (grouped products, Newton-Schulz products).
+//
+// A tile is 128 CG rows x BN columns (CG = 2: a pair of CTAs shares one tcgen05.mma.cta_group::2, each CTA holds its own 128 rows
+// of A, half of the columns of B and the accumulators of its rows).  The inner dimension comes in blocks of 64 elements, 128 bytes:
+//   K-major operand:  boxes of 64 rows, 128 bytes of K each
+//   MN-major operand: boxes of 64 inner indices, 128 bytes of consecutive rows each
+// both 8 KiB, 128-byte swizzle; out-of-range elements are read as zero.
+//
+// PLANES = 2: an operand is the sum of two 16-bit planes hi + lo; a stage holds both of A and both of B, and a block takes the three
+// products lo hi, hi lo, hi hi into one accumulator (lo lo is below the last bit of what the planes keep).
+//
+// Accumulation.  The tensor core cuts its running sum off at 24 bits with every instruction, 16 inner indices, which on long sums costs
+// bits that FP32 results would show.  So the sum is cut into segments of seg blocks, each with an accumulator of its own
+// (two slots in turn), which the epilogue warps add up in registers, rounding to nearest.
+//
+// A persistent CTA of 19 warps per multiprocessor:
+//   warp 0       bulk copies into a ring of shared memory (no multicast)
+//   warp 1       issues the MMAs (of a pair: the leader's)
+//   warp 2       RAGGED_K: zeroes, in the last block of a tile, the inner indices that belong to the next group, in both operands
+//                (zeroing one would leave 0 x NaN)
+//   warps 3..18  epilogue, four per lane quarter of the tensor memory, BN / 4 columns each
+// Every wait is bounded: when one runs out the CTA reports OZ_ERR_TIMEOUT, leaves its loops, frees its tensor memory and returns.
+//
+// The tensor memory is taken after dependency_wait() and the successor let in after that: a CTA that waits for its predecessor
+// holds none of what the predecessor still has to take.
+#pragma once
+
+#include "oz_tcgen05.cuh"
+
+namespace oz {
+
+constexpr int P16_THREADS = 19 * 32;
+constexpr int P16_FIRST_EPI = 3;
+constexpr int P16_EPI_WARPS = 16;
+constexpr int P16_BLOCK_K = 64;                    // elements: 128 bytes
+constexpr int P16_BOX_BYTES = 64 * 128;
+constexpr int P16_RING_BYTES = 192 * 1024;
+constexpr int P16_BARRIER_BYTES = 512;
+
+template <int CG, int BN, int PLANES>
+struct Ring16 {
+    static constexpr int B_ROWS = BN / CG;                                   // columns of the tile that one CTA loads
+    static constexpr int B_BOX_ROWS = B_ROWS < 64 ? B_ROWS : 64;
+    static constexpr int B_BOXES = B_ROWS / B_BOX_ROWS;
+    static constexpr int B_BOX_BYTES = B_BOX_ROWS * 128;
+    static constexpr int A_PLANE = 2 * P16_BOX_BYTES;
+    static constexpr int B_PLANE = B_BOXES * B_BOX_BYTES;
+    static constexpr int STAGE = PLANES * (A_PLANE + B_PLANE);
+    static constexpr int STAGES = P16_RING_BYTES / STAGE;
+    static constexpr int COLS = BN / 4;                                      // columns of an epilogue warp
+    static_assert(24 * STAGES + 40 <= P16_BARRIER_BYTES, "barriers");
+};
+
+// what the roles need to know of a launch and of a tile, whatever the policy
+struct Core16 {
+    uint32_t idesc;             // instruction descriptor without the number of columns
+    int a_mn, b_mn;             // operand stored along its rows (MN-major)
+    int plane_z;                // third coordinate from one plane to the next
+    int seg;                    // blocks per accumulator
+    unsigned int *status;
+};
+struct Tile16 {
+    int a_row, a_z, b_row, b_z; // coordinates of the tile's first row of A and column of B
+    int k_begin, k_len;
+    int cols;                   // columns computed: a multiple of 16 CG
+};
+
+inline uint32_t idesc16(bool bf16, bool a_mn, bool b_mn, int cg)
+{
+    const uint32_t fmt = bf16 ? 1u : 0u;
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | (static_cast<uint32_t>(a_mn) << 15) | (static_cast<uint32_t>(b_mn) << 16) |
+           (static_cast<uint32_t>((128 * cg) >> 4) << 24);
+}
+
+template <int CG>
+__device__ __forceinline__ void umma16(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate)
+{
+    if constexpr (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(da), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+
+// shared-memory descriptor of a plane of an operand.  K-major: groups of 8 rows 1024 bytes apart.  MN-major: groups of 8 inner
+// indices 1024 bytes apart (stride), the next 64 rows in the next box (leading).
+__device__ __forceinline__ uint64_t smem_desc16(uint32_t addr, int mn)
+{
+    const uint64_t leading = mn ? P16_BOX_BYTES >> 4 : 1;
+    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (leading << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
+           (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+}
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// arrivals at a barrier of any CTA of the cluster, ordered after this thread's (and, through it, its warp's) writes
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cluster_addr, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_addr), "r"(bytes) : "memory");
+}
+
+// Policy P:
+//   P::Params              the launch: has a Core16 `core`
+//   P::Tile                a tile: derives from Tile16
+//   P::RAGGED_K            k_begin and k_len are any numbers, and what lies behind them must not enter (MN-major operands only)
+//   P::setup(p, table)     all threads, after the predecessor's end: what `table`, shared memory of the launch's choice, holds
+//   P::total(p, table)     number of tiles
+//   P::decode<CG, BN>(p, table, item)
+//   P::store<CG, BN>(p, tile, acc, row, col): the thread's results, row of the tile (0 .. 128 CG - 1), columns col .. col + BN / 4 - 1
+template <class P, int CG, int BN, int PLANES>
+__global__ void __launch_bounds__(P16_THREADS, 1)
+product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+                 const __grid_constant__ typename P::Params p)
+{
+    using R = Ring16<CG, BN, PLANES>;
+    constexpr int STAGES = R::STAGES;
+    constexpr int TMEM_COLUMNS = 2 * BN < 32 ? 32 : 2 * BN;
+    const uint32_t rank = CG == 2 ? cluster_ctarank() : 0u;
+    const int64_t first_item = CG == 2 ? (blockIdx.x >> 1) : blockIdx.x;
+    const int64_t item_step = CG == 2 ? (gridDim.x >> 1) : gridDim.x;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t ring = (raw + 1023u) & ~1023u;
+    const uint32_t full_bar = ring + P16_RING_BYTES;            // STAGES x 8 bytes each
+    const uint32_t empty_bar = full_bar + 8 * STAGES;
+    const uint32_t tail_bar = empty_bar + 8 * STAGES;
+    const uint32_t tfull_bar = tail_bar + 8 * STAGES;           // 2 x 8
+    const uint32_t tempty_bar = tfull_bar + 16;                 // 2 x 8
+    unsigned char *gen = smem_raw + (ring - raw) + P16_RING_BYTES;
+    volatile uint32_t *tmem_base_ptr = reinterpret_cast<volatile uint32_t *>(gen + 24 * STAGES + 32);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 24 * STAGES + 36);
+    int *table = reinterpret_cast<int *>(gen + P16_BARRIER_BYTES);
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        prefetch_map(&mapA);
+        prefetch_map(&mapB);
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(full_bar + 8 * s, CG);                    // a CTA's copies, or what zeroes behind them, arrive once
+            mbar_init(empty_bar + 8 * s, 1);
+            mbar_init(tail_bar + 8 * s, 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(tfull_bar + 8 * s, 1);
+            mbar_init(tempty_bar + 8 * s, P16_EPI_WARPS * CG);
+        }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    dependency_wait();
+    if (warp == 1) tmem_alloc<CG>(smem_u32(const_cast<uint32_t *>(tmem_base_ptr)), TMEM_COLUMNS);
+    P::setup(p, BN, table);
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync_all();          // the peer's barriers exist before anything signals them
+    tc_fence_after();
+    dependency_release();
+    const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_base_ptr, 0);
+    const int64_t total = P::template total<CG, BN>(p, table);
+    unsigned int *const status = p.core.status;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
+    auto needs_tail = [&](const Tile16 &t) { return P::RAGGED_K && (t.k_len & 15) != 0; };
+
+    if (warp < P16_FIRST_EPI) {
+        // whole warps walk the loops, one elected lane issues: addresses and descriptors stay in uniform registers
+        const bool leader = elect_one();
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        if (warp == 0) {
+            // -------------------------------------------------------- copies
+            for (int64_t item = first_item; ok && item < total; item += item_step) {
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
+                const int b_rows = t.cols / CG, b_boxes = R::B_BOXES == 1 ? 1 : (b_rows + 63) >> 6;
+                const int a_row = t.a_row + static_cast<int>(rank) * 128, b_row = t.b_row + static_cast<int>(rank) * b_rows;
+                const uint32_t bytes = PLANES * (R::A_PLANE + b_boxes * R::B_BOX_BYTES);
+                for (int kb = 0; ok && kb < blocks; ++kb) {
+                    ok = wait(empty_bar + 8 * stage, phase ^ 1u);
+                    if (!ok) break;
+                    const int kk = t.k_begin + kb * P16_BLOCK_K;
+                    const uint32_t sa = ring + stage * R::STAGE, sb = sa + PLANES * R::A_PLANE;
+                    const bool tail = needs_tail(t) && kb == blocks - 1;
+                    if (leader) {
+                        uint32_t bar;
+                        if (CG == 1) {
+                            bar = (tail ? tail_bar : full_bar) + 8 * stage;
+                            mbar_expect_tx(bar, bytes);
+                        } else {
+                            bar = tail ? map_to_cta(tail_bar + 8 * stage, rank) : map_to_cta(full_bar + 8 * stage, 0);
+                            mbar_expect_tx_cluster(bar, bytes);
+                        }
+                        auto copy = [&](uint32_t dst, const CUtensorMap *map, int mn, int row, int z) {
+                            const int c0 = mn ? row : kk, c1 = mn ? kk : row;
+                            if (CG == 1) tma_load_3d(dst, map, bar, c0, c1, z);
+                            else tma_load_3d_pair(dst, map, bar, c0, c1, z);
+                        };
+#pragma unroll
+                        for (int pl = 0; pl < PLANES; ++pl) {
+#pragma unroll
+                            for (int b = 0; b < 2; ++b)
+                                copy(sa + pl * R::A_PLANE + b * P16_BOX_BYTES, &mapA, p.core.a_mn, a_row + 64 * b, t.a_z + pl * p.core.plane_z);
+#pragma unroll
+                            for (int b = 0; b < R::B_BOXES; ++b)
+                                if (b < b_boxes)
+                                    copy(sb + pl * R::B_PLANE + b * R::B_BOX_BYTES, &mapB, p.core.b_mn, b_row + 64 * b, t.b_z + pl * p.core.plane_z);
+                        }
+                    }
+                    if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                }
+            }
+        } else if (warp == 1 && rank == 0) {
+            // -------------------------------------------------------- MMAs
+            const uint32_t step_a = p.core.a_mn ? 2048 >> 4 : 32 >> 4, step_b = p.core.b_mn ? 2048 >> 4 : 32 >> 4;   // 16 inner indices on
+            int slot = 0;
+            uint32_t slot_phase = 0;
+            for (int64_t item = first_item; ok && item < total; item += item_step) {
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
+                const uint32_t idesc = p.core.idesc | (static_cast<uint32_t>(t.cols >> 3) << 17);
+                for (int kb0 = 0; ok && kb0 < blocks; kb0 += p.core.seg) {
+                    ok = wait(tempty_bar + 8 * slot, ((slot_phase >> slot) & 1u) ^ 1u);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d = tmem_base + static_cast<uint32_t>(slot * BN);
+                    const int kb1 = min(blocks, kb0 + p.core.seg);
+                    for (int kb = kb0; kb < kb1; ++kb) {
+                        ok = wait(full_bar + 8 * stage, phase);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t sa = ring + stage * R::STAGE, sb = sa + PLANES * R::A_PLANE;
+                        const uint64_t a = smem_desc16(sa, p.core.a_mn), b = smem_desc16(sb, p.core.b_mn);
+                        const int left = t.k_len - kb * P16_BLOCK_K;
+                        if (leader) {
+                            if constexpr (PLANES == 2) {
+                                constexpr uint64_t a_lo = R::A_PLANE >> 4, b_lo = R::B_PLANE >> 4;
+#pragma unroll
+                                for (int ks = 0; ks < 4; ++ks)
+                                    if (ks * 16 < left) {
+                                        umma16<CG>(d, a + a_lo + ks * step_a, b + ks * step_b, idesc, kb > kb0 || ks > 0 ? 1u : 0u);
+                                        umma16<CG>(d, a + ks * step_a, b + b_lo + ks * step_b, idesc, 1u);
+                                    }
+#pragma unroll
+                                for (int ks = 0; ks < 4; ++ks)
+                                    if (ks * 16 < left) umma16<CG>(d, a + ks * step_a, b + ks * step_b, idesc, 1u);
+                            } else {
+#pragma unroll
+                                for (int ks = 0; ks < 4; ++ks)
+                                    if (ks * 16 < left) umma16<CG>(d, a + ks * step_a, b + ks * step_b, idesc, kb > kb0 || ks > 0 ? 1u : 0u);
+                            }
+                            umma_commit<CG>(empty_bar + 8 * stage);
+                        }
+                        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    if (leader) umma_commit<CG>(tfull_bar + 8 * slot);
+                    slot_phase ^= 1u << slot;
+                    slot ^= 1;
+                }
+            }
+        } else if (P::RAGGED_K && warp == 2) {
+            // -------------------------------------------------------- inner indices behind the group's end
+            uint32_t tail_phase = 0;                         // bit s: phase of stage s's tail barrier
+            for (int64_t item = first_item; ok && item < total; item += item_step) {
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
+                const int last = (stage + blocks - 1) % STAGES;
+                stage = (stage + blocks) % STAGES;
+                if (!needs_tail(t)) continue;
+                ok = wait(tail_bar + 8 * last, (tail_phase >> last) & 1u);
+                if (!ok) break;
+                tail_phase ^= 1u << last;
+                const int from = t.k_len & 63, to = (from + 15) & ~15;
+                const int boxes = 2 + (t.cols / CG + 63) / 64;
+                static_assert(!P::RAGGED_K || (PLANES == 1 && R::B_BOX_ROWS == 64), "ragged inner dimension: one plane, whole boxes");
+                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+                // a row of a box is one inner index: its eight chunks of 16 bytes stay in the row under the swizzle
+                for (int e = lane; e < boxes * (to - from) * 8; e += 32) {
+                    const int chunk = e & 7, row = from + (e >> 3) % (to - from), box = (e >> 3) / (to - from);
+                    *reinterpret_cast<uint4 *>(smem_raw + (ring - raw) + last * R::STAGE + box * P16_BOX_BYTES + row * 128 + chunk * 16) = zero;
+                }
+                asm volatile("fence.proxy.async;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 1) mbar_arrive(full_bar + 8 * last);
+                    else mbar_arrive_cluster(map_to_cta(full_bar + 8 * last, 0));
+                }
+            }
+        }
+        if (!ok) {
+            // give copies and MMAs in flight a bounded time to land before the CTA exits
+            const unsigned long long t0 = global_timer_ns();
+            while (global_timer_ns() - t0 < 2000000ull) { }
+        }
+    } else {
+        // ------------------------------------------------------------ epilogue
+        constexpr int W = R::COLS < 16 ? 8 : 16;             // columns of a load: the running sums and these stay within the registers
+        const int q = warp & 3;                              // lane quarter of the tensor memory
+        const int part = (warp - P16_FIRST_EPI) >> 2;        // BN / 4 of the tile's columns
+        int slot = 0;
+        uint32_t slot_phase = 0;
+        bool ok = true;
+        for (int64_t item = first_item; ok && item < total; item += item_step) {
+            const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+            const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
+            float acc[R::COLS];
+#pragma unroll
+            for (int c = 0; c < R::COLS; ++c) acc[c] = 0.0f;
+            for (int kb0 = 0; ok && kb0 < blocks; kb0 += p.core.seg) {
+                ok = wait(tfull_bar + 8 * slot, (slot_phase >> slot) & 1u);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(slot * BN + part * R::COLS);
+#pragma unroll
+                for (int c0 = 0; c0 < R::COLS; c0 += W) {
+                    if (part * R::COLS + c0 >= t.cols) break;
+                    uint32_t v[W];
+                    if constexpr (W == 16) tmem_ld16(taddr + c0, v);
+                    else tmem_ld8(taddr + c0, v);
+#pragma unroll
+                    for (int c = 0; c < W; ++c) acc[c0 + c] += __uint_as_float(v[c]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 1) mbar_arrive_relaxed(tempty_bar + 8 * slot);
+                    else mbar_arrive_cluster_relaxed(map_to_cta(tempty_bar + 8 * slot, 0));
+                }
+                slot_phase ^= 1u << slot;
+                slot ^= 1;
+            }
+            if (!ok) break;
+            P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS);
+        }
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (CG == 2) cluster_sync_all();          // neither CTA leaves while the other may still touch it
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc<CG>(tmem_base, TMEM_COLUMNS);
+    }
+}
+
+// Map over 16-bit elements [z][line][inner], box = 64 elements x box_lines lines, 128-byte swizzle, out-of-range elements read as zero.
+// False where the driver does not take these strides.
+inline bool make_map16(CUtensorMap *map, bool bf16, const void *base, int64_t inner, int64_t lines, int64_t ld, int64_t z, int64_t stride, int box_lines)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn || ld >= (1ll << 38) || stride >= (1ll << 38)) return false;
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(lines), static_cast<cuuint64_t>(z)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(2 * ld), static_cast<cuuint64_t>(2 * stride)};
+    cuuint32_t box[3] = {static_cast<cuuint32_t>(P16_BLOCK_K), static_cast<cuuint32_t>(box_lines), 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box,
+              estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class P, int CG, int BN, int PLANES>
+oz_status_t launch_product16(const CUtensorMap &mapA, const CUtensorMap &mapB, const typename P::Params &p, int64_t most_tiles,
+                             size_t table_bytes, cudaStream_t stream)
+{
+    auto kernel = product16_kernel<P, CG, BN, PLANES>;
+    static std::atomic<unsigned long long> ready{0};
+    // (one request for the largest table: the shared memory that a kernel may take is set once a device)
+    OZ_CUDA_CHECK(allow_shared(kernel, kMaxShared, ready));
+    int64_t groups = sm_count() / CG;
+    if (most_tiles < groups) groups = most_tiles;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(groups * CG));
+    cfg.blockDim = dim3(P16_THREADS);
+    cfg.dynamicSmemBytes = P16_RING_BYTES + 1024 + P16_BARRIER_BYTES + table_bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    OZ_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, mapA, mapB, p));
+    count_launch();
+    return OZ_OK;
+}
+
+}  // namespace oz
