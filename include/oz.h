@@ -364,6 +364,25 @@ oz_status_t oz_gemm_grouped_wgrad(int64_t m, int64_t n, int64_t tokens, int64_t 
                                   oz_type_t ctype, double beta, void *C, int64_t ldc, int64_t strideC,
                                   void *stream);
 
+/* Orthogonalising an update by Newton-Schulz products (the Muon optimiser's step on a matrix parameter), for `count` matrices:
+ *     X = G / (|G|_F + eps), then `steps` times   X <- a X + (b S + c S S) X,   S = X X^T,    O = X,
+ * with {a, b, c} = coefficients (HOST array); every step takes the singular values s of X to a s + b s^3 + c s^5.  G_i = G + i strideG and
+ * O_i = O + i strideO are m x n, column-major (ldg, ldo >= m; strides in elements; with several matrices strideO >= ldo (n - 1) + m).
+ * The update of the transpose is the transpose of the update, so row-major matrices are passed as their transposes.
+ * type, otype: OZ_BF16, OZ_F16 or OZ_F32 each.  Iterates and products keep 22 bits and FP32 sums whatever the types (see
+ * csrc/oz_orthogonalise.cu); the result is rounded once.  A matrix of zeros gives zeros, one that holds Inf or NaN gives NaN throughout and sets
+ * OZ_ERR_NONFINITE_INPUT; the matrices of a call do not touch one another.  The same call gives the same bits in every run.
+ * O may be G itself with the same type, leading dimension and stride.
+ * workspace: DEVICE memory of the caller, 256-byte aligned, at least oz_orthogonalise_workspace_bytes(m, n, count) bytes (0 where that is 0),
+ * whose content means nothing before and after; calls that may run at the same time need one each.
+ * OZ_ERR_UNSUPPORTED: more than 100 steps; coefficients that take the largest possible singular value above 2^30 or below 2^-30 on the
+ * way; more than 2^38 elements. */
+size_t oz_orthogonalise_workspace_bytes(int64_t m, int64_t n, int64_t count);
+oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type, const void *G, int64_t ldg,
+                             int64_t strideG, int steps, const double *coefficients, double eps,
+                             oz_type_t otype, void *O, int64_t ldo, int64_t strideO, void *workspace,
+                             size_t bytes, void *stream);
+
 /* Optional per-stage timing hook for benchmarks (the paper's Algorithm 1 prices each stage
  * separately), kept per device: it applies to the device that is current when it is set.  `events`
  * is a HOST array of 5 cudaEvent_t handles (as void*), or NULL to switch the hook off.  While set,

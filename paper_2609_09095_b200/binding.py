@@ -35,6 +35,7 @@ EXPORTS = ["oz_set_info", "oz_plane_count", "oz_plane_count_side", "oz_row_pitch
            "oz_dgemm_ex", "oz_dgemm_host", "oz_operand_bytes", "oz_product_workspace_bytes", "oz_prepare_operand",
            "oz_dgemm_prepared", "oz_deconstruct", "oz_deconstruct_static",
            "oz_residue_gemm", "oz_reconstruct", "oz_gemm_grouped", "oz_gemm_grouped_wgrad",
+           "oz_orthogonalise_workspace_bytes", "oz_orthogonalise",
            "oz_query_status", "oz_query_fallback_rows", "oz_set_stage_events", "oz_launch_count", "oz_status_string"]
 
 __all__ = EXPORTS + ["EXPORTS", "OzError", "load", "check", "LIB_PATH", "OZ_OK", "OZ_ERR_INVALID_ARG",
@@ -88,6 +89,9 @@ def load() -> C.CDLL:
     lib.oz_reconstruct.argtypes = [i64, i64, vp, i64, i64, vp, vp, i32, dbl, dbl, vp, i64, vp]
     lib.oz_gemm_grouped.argtypes = [i32, i64, i64, i64, i64, vp, i32, vp, i64, i64, vp, i64, i32, dbl, vp, i64, vp]
     lib.oz_gemm_grouped_wgrad.argtypes = [i64, i64, i64, i64, vp, i32, vp, i64, vp, i64, i32, dbl, vp, i64, i64, vp]
+    lib.oz_orthogonalise_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.oz_orthogonalise_workspace_bytes.restype = C.c_size_t
+    lib.oz_orthogonalise.argtypes = [i64, i64, i64, i32, vp, i64, i64, i32, C.POINTER(dbl), dbl, i32, vp, i64, i64, vp, C.c_size_t, vp]
     lib.oz_query_status.argtypes = [vp]
     lib.oz_query_fallback_rows.argtypes = [vp, C.POINTER(C.c_int64)]
     lib.oz_set_stage_events.argtypes = [C.POINTER(vp)]
@@ -234,6 +238,20 @@ def oz_gemm_grouped(transA, m, n, k, groups, offsets, dtype, A, lda, strideA, B,
 def oz_gemm_grouped_wgrad(m, n, tokens, groups, offsets, dtype, A, lda, B, ldb, ctype, beta, Cm, ldc, strideC, stream=None) -> int:
     return load().oz_gemm_grouped_wgrad(m, n, tokens, groups, _ptr(offsets), dtype, _ptr(A), lda, _ptr(B), ldb, ctype, beta,
                                         _ptr(Cm), ldc, strideC, _stream(stream))
+
+
+def oz_orthogonalise_workspace_bytes(m, n, count=1) -> int:
+    return load().oz_orthogonalise_workspace_bytes(m, n, count)
+
+
+def oz_orthogonalise(m, n, count, dtype, G, ldg, strideG, steps, coefficients, eps, otype, O, ldo, strideO, workspace, nbytes=None,
+                     stream=None) -> int:
+    """coefficients: the three numbers a, b, c, or None with steps = 0."""
+    if nbytes is None:
+        nbytes = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    abc = None if coefficients is None else (C.c_double * 3)(*coefficients)
+    return load().oz_orthogonalise(m, n, count, dtype, _ptr(G), ldg, strideG, steps, abc, eps, otype, _ptr(O), ldo, strideO, _ptr(workspace), nbytes,
+                                   _stream(stream))
 
 
 def oz_query_status(stream=None) -> int:
