@@ -18,7 +18,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "oz_product16.cuh"
 
@@ -36,6 +38,11 @@ __device__ __forceinline__ float load_number(const void *X, int64_t at, int type
     if (type == OZ_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(X)[at]);
     return __half2float(static_cast<const __half *>(X)[at]);
 }
+
+template <class T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ float from_float(float v) { return v; }
 
 __device__ __forceinline__ void store_number(void *X, int64_t at, float v, int type)
 {
@@ -213,38 +220,91 @@ struct NewtonPolicy {
         return t;
     }
 
+    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and BN / 4 columns, eight at a time.
     template <int CG, int BN>
     static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[BN / 4], int row, int col)
     {
-        const int i = t.a_row + row, j0 = t.j0 + col, lines = SYMMETRIC ? p.r : p.c;
-        if (i >= p.r || j0 >= lines) return;
+        const int i = t.a_row + row, j0 = t.j0 + col, lines = SYMMETRIC ? p.r : p.c, left = lines - j0;
+        if (i >= p.r || left <= 0) return;
         const int64_t plane = static_cast<int64_t>(lines) * p.rp, base = t.matrix * 2 * plane, at = base + i + static_cast<int64_t>(j0) * p.rp;
+        const __half *old = p.old + at;
+        // eight results: alpha accumulator + beta old
+        auto results = [&](float (&v)[8], int c0) {
+            float was[8];
+            if constexpr (MODE != kGram) {
 #pragma unroll
-        for (int c0 = 0; c0 < BN / 4; c0 += 8) {
-            __align__(16) __half hi[8], lo[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const bool inside = j0 + c0 + c < lines;
-                const int64_t e = at + static_cast<int64_t>(c0 + c) * p.rp;
-                float v = p.alpha * acc[c0 + c];
-                if (MODE != kGram && inside) v = fmaf(p.beta, __half2float(p.old[e]) + __half2float(p.old[e + plane]), v);
-                if (MODE == kApplyLast) {
-                    if (inside)
-                        store_number(p.O, t.matrix * p.strideO + (p.transposed ? j0 + c0 + c + i * p.ldo : i + (j0 + c0 + c) * p.ldo), v, p.otype);
-                } else {
-                    split_planes(v, &hi[c], &lo[c]);
-                    if (inside) {
-                        p.out[e] = hi[c];
-                        p.out[e + plane] = lo[c];
-                    }
+                for (int c = 0; c < 8; ++c) {
+                    was[c] = c0 + c < left ? __half2float(old[0]) + __half2float(old[plane]) : 0.0f;
+                    old += p.rp;
                 }
             }
-            if (SYMMETRIC) {
-                // rows j0 .. of column i: aligned, and what lies between r and rp is nobody's
-                if (t.mirror && j0 + c0 < lines) {
-                    __half *to = p.out + base + (j0 + c0) + static_cast<int64_t>(i) * p.rp;
-                    *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(hi);
-                    *reinterpret_cast<uint4 *>(to + plane) = *reinterpret_cast<const uint4 *>(lo);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = MODE == kGram ? p.alpha * acc[c0 + c] : fmaf(p.beta, was[c], p.alpha * acc[c0 + c]);
+        };
+        if constexpr (MODE == kApplyLast) {
+            auto as = [&](auto *O) {
+                using T = typename std::remove_pointer<decltype(O)>::type;
+                O += t.matrix * p.strideO;
+                if (p.transposed) {
+                    // the row's elements are consecutive
+                    T *to = O + j0 + i * p.ldo;
+                    const bool wide = reinterpret_cast<uintptr_t>(to) % 16 == 0;
+#pragma unroll
+                    for (int c0 = 0; c0 < BN / 4; c0 += 8) {
+                        float v[8];
+                        results(v, c0);
+                        if (wide && c0 + 8 <= left) {
+                            __align__(16) T w[8];
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) w[c] = from_float<T>(v[c]);
+#pragma unroll
+                            for (int c = 0; c < static_cast<int>(8 * sizeof(T)) / 16; ++c)
+                                reinterpret_cast<uint4 *>(to + c0)[c] = reinterpret_cast<const uint4 *>(w)[c];
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 8; ++c)
+                                if (c0 + c < left) to[c0 + c] = from_float<T>(v[c]);
+                        }
+                    }
+                } else {
+                    T *to = O + i + j0 * p.ldo;
+#pragma unroll
+                    for (int c0 = 0; c0 < BN / 4; c0 += 8) {
+                        float v[8];
+                        results(v, c0);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            if (c0 + c < left) *to = from_float<T>(v[c]);
+                            to += p.ldo;
+                        }
+                    }
+                }
+            };
+            if (p.otype == OZ_F32) as(static_cast<float *>(p.O));
+            else if (p.otype == OZ_BF16) as(static_cast<__nv_bfloat16 *>(p.O));
+            else as(static_cast<__half *>(p.O));
+        } else {
+            __half *to = p.out + at;
+            // the same elements of the other triangle: rows j0 .. of column i, aligned, and what lies between r and rp is nobody's
+            __half *mirror = p.out + base + j0 + static_cast<int64_t>(i) * p.rp;
+#pragma unroll
+            for (int c0 = 0; c0 < BN / 4; c0 += 8) {
+                float v[8];
+                __align__(16) __half hi[8], lo[8];
+                results(v, c0);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) split_planes(v[c], &hi[c], &lo[c]);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    if (c0 + c < left) {
+                        to[0] = hi[c];
+                        to[plane] = lo[c];
+                    }
+                    to += p.rp;
+                }
+                if (SYMMETRIC && t.mirror && c0 < left) {
+                    *reinterpret_cast<uint4 *>(mirror + c0) = *reinterpret_cast<const uint4 *>(hi);
+                    *reinterpret_cast<uint4 *>(mirror + c0 + plane) = *reinterpret_cast<const uint4 *>(lo);
                 }
             }
         }
