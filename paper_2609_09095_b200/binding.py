@@ -111,10 +111,16 @@ def _ptr(t) -> int:
     return t.data_ptr()
 
 
+_torch = None
+
+
 def _stream(stream) -> int:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        # the handle itself: building a stream object for it takes longer than a launch
+        global _torch
+        if _torch is None:
+            import torch as _torch
+        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -293,19 +293,19 @@ struct GroupedPolicy {
         return t;
     }
 
-    template <int CG, int BN>
-    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[BN / 4], int row, int col)
+    template <int CG, int BN, int N>
+    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col)
     {
         if (row >= t.rows || (t.k_len == 0 && p.accumulate)) return;
         store_row(p.C, t.c + row + col * p.ldc, p.ldc, acc, t.valid - col, p.ctype, p.accumulate);
     }
 };
 
-template <bool INNER, int CG, int BN>
+template <bool INNER, int CG, int BN, int SPLIT = 1>
 oz_status_t launch_tiles(GroupedParams &p, bool bf16, const CUtensorMap &mapA, const CUtensorMap &mapB, int64_t most, cudaStream_t stream)
 {
     p.core.idesc = idesc16(bf16, p.core.a_mn, p.core.b_mn, CG);
-    return launch_product16<GroupedPolicy<INNER>, CG, BN, 1>(mapA, mapB, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
+    return launch_product16<GroupedPolicy<INNER>, CG, BN, 1, SPLIT>(mapA, mapB, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
 }
 
 // tiles of 128 cg x bn at most: what the host knows of the groups is their number and that of all columns
@@ -331,7 +331,6 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
     const bool bf16 = type == OZ_BF16;
     p.core.a_mn = p.rowA == 1 && p.innerA != 1;
     p.core.b_mn = INNER;
-    p.core.plane_z = 0;
     p.core.status = p.status;
     // sums that become 16-bit numbers need no segments
     p.core.seg = p.ctype == OZ_F32 ? 4 : 1 << 24;

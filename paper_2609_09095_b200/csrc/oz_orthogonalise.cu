@@ -9,6 +9,9 @@
 // other three go into one accumulator (PLANES = 2 of the product core).  Elements above 2^-18 of the bound keep all 22 bits, smaller ones an
 // absolute 2^-40 of it.
 //
+// Planes in memory: [matrix][line][chunk of 64 elements][hi, lo][64], so that both halves of an element lie at a fixed distance, and a block
+// of an operand is the same box whether its lines or its elements are the inner dimension.  Elements behind the last are zero.
+//
 // S and P are symmetric: only tiles on and below the diagonal are computed, those below are stored twice.  (Tiles on it are stored
 // as computed.)  X keeps its r rows consecutive: for X X^T it is an operand stored along its rows, for P X one stored along the inner dimension,
 // both by the same bulk copies, and S and P are read along whichever direction suits.
@@ -64,14 +67,17 @@ struct MatrixParams {
     void *O;
     int type, otype;
     int transposed;                 // m > n: X is the transpose of G
-    int r, c, rp;                   // X is r x c, r <= c, its columns rp elements apart
+    int r, c, ld;                   // X is r x c, r <= c, its columns ld half-precision numbers apart
     int parts;
     double *sums;                   // [count][parts]
     double eps;
     float scale;                    // of the planes
-    __half *X;                      // [count][2][c][rp]
+    __half *X;                      // plane pairs: [count][c][ld]
     unsigned int *status;
 };
+
+// where element i of a line of plane pairs lies; its lo half is 64 numbers on
+__device__ __forceinline__ int pair_at(int i) { return (i >> 6) * 128 + (i & 63); }
 
 // Sums of squares, in double: any finite FP32 number squares without overflow, and the order is fixed.
 __global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const MatrixParams p)
@@ -142,13 +148,16 @@ __global__ void __launch_bounds__(256) planes_kernel(const MatrixParams p)
     }
     if (!PLANES) return;
     __syncthreads();
-    __half *hi = p.X + matrix * 2 * p.c * p.rp, *lo = hi + static_cast<int64_t>(p.c) * p.rp;
     const int64_t x0 = p.transposed ? j0 : i0, y0 = p.transposed ? i0 : j0;       // first row and column of X
 #pragma unroll
     for (int s = 0; s < PLANE_TILE; s += 4) {
+        // rows behind the last are written too: the tile holds zeros there
         const int64_t x = x0 + ti, y = y0 + tj + s;
         const float v = p.transposed ? tile[ti][tj + s] : tile[tj + s][ti];
-        if (x < p.r && y < p.c) split_planes(v, hi + x + y * p.rp, lo + x + y * p.rp);
+        if (y < p.c) {
+            __half *to = p.X + (matrix * p.c + y) * p.ld + pair_at(static_cast<int>(x));
+            split_planes(v, to, to + 64);
+        }
     }
 }
 
@@ -156,10 +165,10 @@ __global__ void __launch_bounds__(256) planes_kernel(const MatrixParams p)
 enum { kGram, kPolynomial, kApply, kApplyLast };
 
 struct NewtonParams {
-    int count, r, c, rp;
+    int count, r, c, ld;
     float alpha, beta;              // result = alpha accumulator + beta old
-    const __half *old;              // planes [count][2][..][rp]: S of kPolynomial, X of kApply
-    __half *out;                    // planes
+    const __half *old;              // plane pairs [count][r or c][ld]: S of kPolynomial, X of kApply
+    __half *out;                    // plane pairs
     void *O;                        // kApplyLast
     int64_t ldo, strideO;
     int otype, transposed;
@@ -212,34 +221,49 @@ struct NewtonPolicy {
         t.mirror = SYMMETRIC && ti != tj;
         t.a_row = static_cast<int>(ti) * 128 * CG;
         t.b_row = t.j0 = static_cast<int>(tj) * BN;
-        t.a_z = t.b_z = 2 * t.matrix;
+        t.a_z = t.b_z = t.matrix;
         t.k_begin = 0;
         t.k_len = MODE == kGram ? p.c : p.r;
         const int left = (SYMMETRIC ? p.r : p.c) - t.j0;
-        t.cols = left >= BN ? BN : (left + 16 * CG - 1) / (16 * CG) * (16 * CG);
+        // (an operand along its rows comes in whole chunks: half of the columns from each CTA)
+        constexpr int GRAIN = MODE == kGram ? 64 * CG : 16 * CG;
+        t.cols = left >= BN ? BN : (left + GRAIN - 1) / GRAIN * GRAIN;
         return t;
     }
 
-    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and BN / 4 columns, eight at a time.
-    template <int CG, int BN>
-    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[BN / 4], int row, int col)
+    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and N columns, eight at a time at most.
+    template <int CG, int BN, int N>
+    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col)
     {
         const int i = t.a_row + row, j0 = t.j0 + col, lines = SYMMETRIC ? p.r : p.c, left = lines - j0;
-        if (i >= p.r || left <= 0) return;
-        const int64_t plane = static_cast<int64_t>(lines) * p.rp, base = t.matrix * 2 * plane, at = base + i + static_cast<int64_t>(j0) * p.rp;
-        const __half *old = p.old + at;
-        // eight results: alpha accumulator + beta old
-        auto results = [&](float (&v)[8], int c0) {
-            float was[8];
+        if (i >= (MODE == kApplyLast ? p.r : p.ld / 2) || left <= 0) return;
+        if (left >= N) store_columns<true>(p, t, acc, i, j0, lines, left);
+        else store_columns<false>(p, t, acc, i, j0, lines, left);
+    }
+
+    template <bool FULL, int N>
+    static __device__ __forceinline__ void store_columns(const Params &p, const Tile &t, const float (&acc)[N], int i, int j0, int lines, int left)
+    {
+        constexpr int STEP = N < 8 ? N : 8;
+        const int64_t base = static_cast<int64_t>(t.matrix) * lines * p.ld, at = base + static_cast<int64_t>(j0) * p.ld + pair_at(i);
+        const __half *old = MODE == kGram ? nullptr : p.old + at;
+        // some results: alpha accumulator + beta old
+        auto results = [&](float (&v)[STEP], int c0) {
+            __half hi[STEP], lo[STEP];
             if constexpr (MODE != kGram) {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    was[c] = c0 + c < left ? __half2float(old[0]) + __half2float(old[plane]) : 0.0f;
-                    old += p.rp;
+                for (int c = 0; c < STEP; ++c) {
+                    const bool inside = FULL || c0 + c < left;
+                    hi[c] = inside ? old[0] : __half();
+                    lo[c] = inside ? old[64] : __half();
+                    old += p.ld;
                 }
             }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = MODE == kGram ? p.alpha * acc[c0 + c] : fmaf(p.beta, was[c], p.alpha * acc[c0 + c]);
+            for (int c = 0; c < STEP; ++c) {
+                v[c] = p.alpha * acc[c0 + c];
+                if constexpr (MODE != kGram) v[c] = fmaf(p.beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
+            }
         };
         if constexpr (MODE == kApplyLast) {
             auto as = [&](auto *O) {
@@ -247,34 +271,34 @@ struct NewtonPolicy {
                 O += t.matrix * p.strideO;
                 if (p.transposed) {
                     // the row's elements are consecutive
+                    constexpr int WIDE = STEP * static_cast<int>(sizeof(T)) / 16;
                     T *to = O + j0 + i * p.ldo;
-                    const bool wide = reinterpret_cast<uintptr_t>(to) % 16 == 0;
+                    const bool wide = FULL && reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll
-                    for (int c0 = 0; c0 < BN / 4; c0 += 8) {
-                        float v[8];
+                    for (int c0 = 0; c0 < N; c0 += STEP) {
+                        float v[STEP];
                         results(v, c0);
-                        if (wide && c0 + 8 <= left) {
-                            __align__(16) T w[8];
+                        __align__(16) T w[STEP];
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) w[c] = from_float<T>(v[c]);
+                        for (int c = 0; c < STEP; ++c) w[c] = from_float<T>(v[c]);
+                        if (WIDE > 0 && wide) {
 #pragma unroll
-                            for (int c = 0; c < static_cast<int>(8 * sizeof(T)) / 16; ++c)
-                                reinterpret_cast<uint4 *>(to + c0)[c] = reinterpret_cast<const uint4 *>(w)[c];
+                            for (int c = 0; c < WIDE; ++c) reinterpret_cast<uint4 *>(to + c0)[c] = reinterpret_cast<const uint4 *>(w)[c];
                         } else {
 #pragma unroll
-                            for (int c = 0; c < 8; ++c)
-                                if (c0 + c < left) to[c0 + c] = from_float<T>(v[c]);
+                            for (int c = 0; c < STEP; ++c)
+                                if (FULL || c0 + c < left) to[c0 + c] = w[c];
                         }
                     }
                 } else {
                     T *to = O + i + j0 * p.ldo;
 #pragma unroll
-                    for (int c0 = 0; c0 < BN / 4; c0 += 8) {
-                        float v[8];
+                    for (int c0 = 0; c0 < N; c0 += STEP) {
+                        float v[STEP];
                         results(v, c0);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) {
-                            if (c0 + c < left) *to = from_float<T>(v[c]);
+                        for (int c = 0; c < STEP; ++c) {
+                            if (FULL || c0 + c < left) *to = from_float<T>(v[c]);
                             to += p.ldo;
                         }
                     }
@@ -285,26 +309,29 @@ struct NewtonPolicy {
             else as(static_cast<__half *>(p.O));
         } else {
             __half *to = p.out + at;
-            // the same elements of the other triangle: rows j0 .. of column i, aligned, and what lies between r and rp is nobody's
-            __half *mirror = p.out + base + j0 + static_cast<int64_t>(i) * p.rp;
+            // The same elements of the other triangle: elements j0 .. of line i, where that is one.  Behind the last column they are the zeros that
+            // belong there.
+            __half *mirror = p.out + base + static_cast<int64_t>(i) * p.ld + pair_at(j0);
+            const bool mirrored = SYMMETRIC && t.mirror && i < lines;
 #pragma unroll
-            for (int c0 = 0; c0 < BN / 4; c0 += 8) {
-                float v[8];
-                __align__(16) __half hi[8], lo[8];
+            for (int c0 = 0; c0 < N; c0 += STEP) {
+                float v[STEP];
+                __align__(16) __half hi[STEP], lo[STEP];
                 results(v, c0);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) split_planes(v[c], &hi[c], &lo[c]);
+                for (int c = 0; c < STEP; ++c) split_planes(v[c], &hi[c], &lo[c]);
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    if (c0 + c < left) {
+                for (int c = 0; c < STEP; ++c) {
+                    if (FULL || c0 + c < left) {
                         to[0] = hi[c];
-                        to[plane] = lo[c];
+                        to[64] = lo[c];
                     }
-                    to += p.rp;
+                    to += p.ld;
                 }
-                if (SYMMETRIC && t.mirror && c0 < left) {
+                static_assert(!SYMMETRIC || STEP == 8, "whole vectors");
+                if (mirrored && (FULL || c0 < left)) {
                     *reinterpret_cast<uint4 *>(mirror + c0) = *reinterpret_cast<const uint4 *>(hi);
-                    *reinterpret_cast<uint4 *>(mirror + c0 + plane) = *reinterpret_cast<const uint4 *>(lo);
+                    *reinterpret_cast<uint4 *>(mirror + c0 + 64) = *reinterpret_cast<const uint4 *>(lo);
                 }
             }
         }
@@ -315,20 +342,20 @@ template <int MODE>
 oz_status_t launch_newton(NewtonParams &p, const CUtensorMap &mapA, const CUtensorMap &mapB, cudaStream_t stream)
 {
     constexpr bool SYMMETRIC = NewtonPolicy<MODE>::SYMMETRIC;
-    auto tiles = [&](int rows, int cols) {
-        const int64_t tm = (p.r + rows - 1) / rows;
-        return p.count * (SYMMETRIC ? tm * (tm + 1) / 2 : tm * ((p.c + cols - 1) / cols));
-    };
+    const int64_t tm = (p.r + 255) / 256, tiles = p.count * (SYMMETRIC ? tm * (tm + 1) / 2 : tm * ((p.c + 255) / 256));
     p.core.a_mn = p.core.b_mn = MODE == kGram;
-    const bool pairs = tiles(256, 256) >= sm_count() / 2;
-    p.core.idesc = idesc16(false, p.core.a_mn, p.core.b_mn, pairs ? 2 : 1);
-    if (pairs) return launch_product16<NewtonPolicy<MODE>, 2, 256, 2>(mapA, mapB, p, tiles(256, 256), 0, stream);
-    return launch_product16<NewtonPolicy<MODE>, 1, 128, 2>(mapA, mapB, p, tiles(128, 128), 0, stream);
+    p.core.idesc = idesc16(false, p.core.a_mn, p.core.b_mn, 2);
+    // Tiles are always 256 x 256 by pairs: the three plane products of a block read shared memory at 106 bytes a cycle; those of tiles of 128 x 128 by
+    // single CTAs would at 213 of the 128 that it has.  Few tiles are shared out along the inner dimension.
+    const int64_t pairs = sm_count() / 2;
+    if (4 * tiles <= pairs) return launch_product16<NewtonPolicy<MODE>, 2, 256, 2, 4>(mapA, mapB, p, tiles, 0, stream);
+    if (2 * tiles <= pairs) return launch_product16<NewtonPolicy<MODE>, 2, 256, 2, 2>(mapA, mapB, p, tiles, 0, stream);
+    return launch_product16<NewtonPolicy<MODE>, 2, 256, 2, 1>(mapA, mapB, p, tiles, 0, stream);
 }
 
 // ---------------------------------------------------------------- host side
 struct Layout {
-    int64_t r, c, rp;
+    int64_t r, c, chunks;
     int parts;
     size_t sums, x[2], s, poly, total;
 };
@@ -338,7 +365,7 @@ Layout layout_of(int64_t m, int64_t n, int64_t count)
     Layout l{};
     l.r = m < n ? m : n;
     l.c = m < n ? n : m;
-    l.rp = round_up(l.r, 8);                       // 16 bytes: the stride of a bulk copy
+    l.chunks = (l.r + 63) / 64;
     const int64_t pieces = (m * n + NORM_THREADS * 16 - 1) / (NORM_THREADS * 16);
     l.parts = static_cast<int>(pieces < MAX_PARTS ? pieces : MAX_PARTS);
     size_t at = 0;
@@ -348,10 +375,10 @@ Layout layout_of(int64_t m, int64_t n, int64_t count)
         return here;
     };
     l.sums = take(count * l.parts * 8);
-    l.x[0] = take(count * 4 * l.c * l.rp);
-    l.x[1] = take(count * 4 * l.c * l.rp);
-    l.s = take(count * 4 * l.r * l.rp);
-    l.poly = take(count * 4 * l.r * l.rp);
+    l.x[0] = take(count * l.c * l.chunks * 256);
+    l.x[1] = take(count * l.c * l.chunks * 256);
+    l.s = take(count * l.r * l.chunks * 256);
+    l.poly = take(count * l.r * l.chunks * 256);
     l.total = at;
     return l;
 }
@@ -399,11 +426,6 @@ double plane_scale(double bound)
     return std::ldexp(1.0, 15 - e);
 }
 
-bool planes_map(CUtensorMap *map, const __half *planes, int64_t lines, const Layout &l, int64_t count)
-{
-    return make_map16(map, false, planes, l.r, lines, l.rp, 2 * count, lines * l.rp, 64);
-}
-
 }  // namespace
 }  // namespace oz
 
@@ -449,8 +471,8 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     __half *x[2] = {reinterpret_cast<__half *>(ws + l.x[0]), reinterpret_cast<__half *>(ws + l.x[1])};
     __half *gram = reinterpret_cast<__half *>(ws + l.s), *poly = reinterpret_cast<__half *>(ws + l.poly);
     CUtensorMap map_x[2], map_s, map_p;
-    if (steps && !(planes_map(&map_x[0], x[0], l.c, l, count) && planes_map(&map_x[1], x[1], l.c, l, count) &&
-                   planes_map(&map_s, gram, l.r, l, count) && planes_map(&map_p, poly, l.r, l, count)))
+    if (steps && !(make_pair_map16(&map_x[0], x[0], l.chunks, l.c, count) && make_pair_map16(&map_x[1], x[1], l.chunks, l.c, count) &&
+                   make_pair_map16(&map_s, gram, l.chunks, l.r, count) && make_pair_map16(&map_p, poly, l.chunks, l.r, count)))
         return OZ_ERR_CUDA;
 
     MatrixParams mp{};
@@ -468,7 +490,7 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     mp.transposed = m > n;
     mp.r = static_cast<int>(l.r);
     mp.c = static_cast<int>(l.c);
-    mp.rp = static_cast<int>(l.rp);
+    mp.ld = static_cast<int>(128 * l.chunks);
     mp.parts = l.parts;
     mp.sums = reinterpret_cast<double *>(ws + l.sums);
     mp.eps = eps;
@@ -485,14 +507,15 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     p.count = static_cast<int>(count);
     p.r = mp.r;
     p.c = mp.c;
-    p.rp = mp.rp;
+    p.ld = mp.ld;
     p.O = O;
     p.ldo = ldo;
     p.strideO = strideO;
     p.otype = otype;
     p.transposed = mp.transposed;
-    p.core.plane_z = 1;
-    p.core.seg = 2;
+    // blocks of 64 an accumulator: error of the result (16 x 512 x 2048, 1024 x 1024) 0.8e-6 and 0.7e-6 with one, 1.4e-6 and 1.2e-6 with two, 5.6e-6
+    // and 3.8e-6 with eight, where a rounding to 16 bits is 1.7e-3 (bfloat16) or 2e-4; the FP32 iteration in one precision has 2e-6 to 5e-6
+    p.core.seg = otype == OZ_F32 ? 2 : 8;
     p.core.status = mp.status;
     for (int step = 0; step < steps; ++step) {
         const double sx = plane_scale(bound[step]), ss = plane_scale(bound[step] * bound[step]),

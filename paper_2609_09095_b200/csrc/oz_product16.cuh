@@ -21,6 +21,11 @@
 //   warp 2       RAGGED_K: zeroes, in the last block of a tile, the inner indices that belong to the next group, in both operands
 //                (zeroing one would leave 0 x NaN)
 //   warps 3..18  epilogue, four per lane quarter of the tensor memory, BN / 4 columns each
+//
+// SPLIT > 1: products of so few tiles that most multiprocessors would have none.  A cluster of SPLIT pairs (or single CTAs) shares one tile, each
+// member a range of the inner dimension; at the end every member owns BN / SPLIT columns, gets the others' sums of them through shared
+// memory of the cluster (in the ring, which nothing fills any more), adds them in the order of the members and stores.  One tile a cluster.
+//
 // Every wait is bounded: when one runs out the CTA reports OZ_ERR_TIMEOUT, leaves its loops, frees its tensor memory and returns.
 //
 // The tensor memory is taken after dependency_wait() and the successor let in after that: a CTA that waits for its predecessor
@@ -41,6 +46,7 @@ constexpr int P16_BARRIER_BYTES = 512;
 
 template <int CG, int BN, int PLANES>
 struct Ring16 {
+    static_assert(P16_EPI_WARPS * 4 * 32 * (BN / 4) <= P16_RING_BYTES, "sums of the other members of a cluster");
     static constexpr int B_ROWS = BN / CG;                                   // columns of the tile that one CTA loads
     static constexpr int B_BOX_ROWS = B_ROWS < 64 ? B_ROWS : 64;
     static constexpr int B_BOXES = B_ROWS / B_BOX_ROWS;
@@ -57,7 +63,6 @@ struct Ring16 {
 struct Core16 {
     uint32_t idesc;             // instruction descriptor without the number of columns
     int a_mn, b_mn;             // operand stored along its rows (MN-major)
-    int plane_z;                // third coordinate from one plane to the next
     int seg;                    // blocks per accumulator
     unsigned int *status;
 };
@@ -114,6 +119,30 @@ __device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cluster_addr, ui
     asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_addr), "r"(bytes) : "memory");
 }
 
+// mbarrier arrives in both CTAs of the pair that begins at cluster rank `pair` once every MMA issued so far by this thread has completed
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint32_t pair)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"(static_cast<uint16_t>(3u << pair)) : "memory");
+}
+
+__device__ __forceinline__ void store_cluster(uint32_t cluster_addr, float v)
+{
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
+}
+
+// 64 elements x 64 lines of a plane of a matrix in plane pairs: (element, chunk and plane, line, matrix)
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar_cluster, int c0, int c1, int c2, int c3)
+{
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar_cluster), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+
 // Policy P:
 //   P::Params              the launch: has a Core16 `core`
 //   P::Tile                a tile: derives from Tile16
@@ -121,8 +150,8 @@ __device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cluster_addr, ui
 //   P::setup(p, table)     all threads, after the predecessor's end: what `table`, shared memory of the launch's choice, holds
 //   P::total(p, table)     number of tiles
 //   P::decode<CG, BN>(p, table, item)
-//   P::store<CG, BN>(p, tile, acc, row, col): the thread's results, row of the tile (0 .. 128 CG - 1), columns col .. col + BN / 4 - 1
-template <class P, int CG, int BN, int PLANES>
+//   P::store<CG, BN>(p, tile, acc, row, col): the thread's results, row of the tile (0 .. 128 CG - 1), as many columns from col on as acc holds
+template <class P, int CG, int BN, int PLANES, int SPLIT>
 __global__ void __launch_bounds__(P16_THREADS, 1)
 product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                  const __grid_constant__ typename P::Params p)
@@ -130,9 +159,11 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     using R = Ring16<CG, BN, PLANES>;
     constexpr int STAGES = R::STAGES;
     constexpr int TMEM_COLUMNS = 2 * BN < 32 ? 32 : 2 * BN;
-    const uint32_t rank = CG == 2 ? cluster_ctarank() : 0u;
-    const int64_t first_item = CG == 2 ? (blockIdx.x >> 1) : blockIdx.x;
-    const int64_t item_step = CG == 2 ? (gridDim.x >> 1) : gridDim.x;
+    const uint32_t place = CG * SPLIT > 1 ? cluster_ctarank() : 0u;
+    const uint32_t rank = place % CG, pair = place - rank;          // in the pair, and the pair's first CTA
+    const int member = static_cast<int>(place / CG);                // of the SPLIT that share a tile
+    const int64_t first_item = blockIdx.x / (CG * SPLIT);
+    const int64_t item_step = gridDim.x / (CG * SPLIT);
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring = (raw + 1023u) & ~1023u;
@@ -167,13 +198,16 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     P::setup(p, BN, table);
     tc_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync_all();          // the peer's barriers exist before anything signals them
+    if (CG * SPLIT > 1) cluster_sync_all();   // the peers' barriers exist before anything signals them
     tc_fence_after();
     dependency_release();
     const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_base_ptr, 0);
     const int64_t total = P::template total<CG, BN>(p, table);
     unsigned int *const status = p.core.status;
     auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
+    // the member's blocks of a tile
+    auto first_block = [&](int blocks) { return SPLIT == 1 ? 0 : static_cast<int>(static_cast<int64_t>(blocks) * member / SPLIT); };
+    auto end_block = [&](int blocks) { return SPLIT == 1 ? blocks : static_cast<int>(static_cast<int64_t>(blocks) * (member + 1) / SPLIT); };
     auto needs_tail = [&](const Tile16 &t) { return P::RAGGED_K && (t.k_len & 15) != 0; };
 
     if (warp < P16_FIRST_EPI) {
@@ -190,7 +224,7 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 const int b_rows = t.cols / CG, b_boxes = R::B_BOXES == 1 ? 1 : (b_rows + 63) >> 6;
                 const int a_row = t.a_row + static_cast<int>(rank) * 128, b_row = t.b_row + static_cast<int>(rank) * b_rows;
                 const uint32_t bytes = PLANES * (R::A_PLANE + b_boxes * R::B_BOX_BYTES);
-                for (int kb = 0; ok && kb < blocks; ++kb) {
+                for (int kb = first_block(blocks), end = end_block(blocks); ok && kb < end; ++kb) {
                     ok = wait(empty_bar + 8 * stage, phase ^ 1u);
                     if (!ok) break;
                     const int kk = t.k_begin + kb * P16_BLOCK_K;
@@ -202,23 +236,27 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                             bar = (tail ? tail_bar : full_bar) + 8 * stage;
                             mbar_expect_tx(bar, bytes);
                         } else {
-                            bar = tail ? map_to_cta(tail_bar + 8 * stage, rank) : map_to_cta(full_bar + 8 * stage, 0);
+                            bar = tail ? map_to_cta(tail_bar + 8 * stage, place) : map_to_cta(full_bar + 8 * stage, pair);
                             mbar_expect_tx_cluster(bar, bytes);
                         }
-                        auto copy = [&](uint32_t dst, const CUtensorMap *map, int mn, int row, int z) {
+                        auto copy = [&](uint32_t dst, const CUtensorMap *map, int mn, int row, int z, int plane) {
                             const int c0 = mn ? row : kk, c1 = mn ? kk : row;
-                            if (CG == 1) tma_load_3d(dst, map, bar, c0, c1, z);
-                            else tma_load_3d_pair(dst, map, bar, c0, c1, z);
+                            if constexpr (PLANES == 2) {
+                                if (CG == 1) tma_load_4d(dst, map, bar, 0, 2 * (c0 >> 6) + plane, c1, z);
+                                else tma_load_4d_pair(dst, map, bar, 0, 2 * (c0 >> 6) + plane, c1, z);
+                            } else {
+                                if (CG == 1) tma_load_3d(dst, map, bar, c0, c1, z);
+                                else tma_load_3d_pair(dst, map, bar, c0, c1, z);
+                            }
                         };
 #pragma unroll
                         for (int pl = 0; pl < PLANES; ++pl) {
 #pragma unroll
                             for (int b = 0; b < 2; ++b)
-                                copy(sa + pl * R::A_PLANE + b * P16_BOX_BYTES, &mapA, p.core.a_mn, a_row + 64 * b, t.a_z + pl * p.core.plane_z);
+                                copy(sa + pl * R::A_PLANE + b * P16_BOX_BYTES, &mapA, p.core.a_mn, a_row + 64 * b, t.a_z, pl);
 #pragma unroll
                             for (int b = 0; b < R::B_BOXES; ++b)
-                                if (b < b_boxes)
-                                    copy(sb + pl * R::B_PLANE + b * R::B_BOX_BYTES, &mapB, p.core.b_mn, b_row + 64 * b, t.b_z + pl * p.core.plane_z);
+                                if (b < b_boxes) copy(sb + pl * R::B_PLANE + b * R::B_BOX_BYTES, &mapB, p.core.b_mn, b_row + 64 * b, t.b_z, pl);
                         }
                     }
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -233,12 +271,12 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
                 const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
                 const uint32_t idesc = p.core.idesc | (static_cast<uint32_t>(t.cols >> 3) << 17);
-                for (int kb0 = 0; ok && kb0 < blocks; kb0 += p.core.seg) {
+                for (int kb0 = first_block(blocks), end = end_block(blocks); ok && kb0 < end; kb0 += p.core.seg) {
                     ok = wait(tempty_bar + 8 * slot, ((slot_phase >> slot) & 1u) ^ 1u);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d = tmem_base + static_cast<uint32_t>(slot * BN);
-                    const int kb1 = min(blocks, kb0 + p.core.seg);
+                    const int kb1 = min(end, kb0 + p.core.seg);
                     for (int kb = kb0; kb < kb1; ++kb) {
                         ok = wait(full_bar + 8 * stage, phase);
                         if (!ok) break;
@@ -263,12 +301,16 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                                 for (int ks = 0; ks < 4; ++ks)
                                     if (ks * 16 < left) umma16<CG>(d, a + ks * step_a, b + ks * step_b, idesc, kb > kb0 || ks > 0 ? 1u : 0u);
                             }
-                            umma_commit<CG>(empty_bar + 8 * stage);
+                            if constexpr (CG == 2) umma_commit_pair(empty_bar + 8 * stage, pair);
+                            else umma_commit<1>(empty_bar + 8 * stage);
                         }
                         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                     }
                     if (!ok) break;
-                    if (leader) umma_commit<CG>(tfull_bar + 8 * slot);
+                    if (leader) {
+                        if constexpr (CG == 2) umma_commit_pair(tfull_bar + 8 * slot, pair);
+                        else umma_commit<1>(tfull_bar + 8 * slot);
+                    }
                     slot_phase ^= 1u << slot;
                     slot ^= 1;
                 }
@@ -279,9 +321,10 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             for (int64_t item = first_item; ok && item < total; item += item_step) {
                 const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
                 const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
-                const int last = (stage + blocks - 1) % STAGES;
-                stage = (stage + blocks) % STAGES;
-                if (!needs_tail(t)) continue;
+                const int mine = end_block(blocks) - first_block(blocks);
+                const int last = (stage + mine - 1) % STAGES;
+                stage = (stage + mine) % STAGES;
+                if (!needs_tail(t) || mine == 0 || end_block(blocks) != blocks) continue;
                 ok = wait(tail_bar + 8 * last, (tail_phase >> last) & 1u);
                 if (!ok) break;
                 tail_phase ^= 1u << last;
@@ -298,7 +341,7 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                 __syncwarp();
                 if (lane == 0) {
                     if (CG == 1) mbar_arrive(full_bar + 8 * last);
-                    else mbar_arrive_cluster(map_to_cta(full_bar + 8 * last, 0));
+                    else mbar_arrive_cluster(map_to_cta(full_bar + 8 * last, pair));
                 }
             }
         }
@@ -307,51 +350,95 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
             const unsigned long long t0 = global_timer_ns();
             while (global_timer_ns() - t0 < 2000000ull) { }
         }
-    } else {
-        // ------------------------------------------------------------ epilogue
-        constexpr int W = R::COLS < 16 ? 8 : 16;             // columns of a load: the running sums and these stay within the registers
-        const int q = warp & 3;                              // lane quarter of the tensor memory
-        const int part = (warp - P16_FIRST_EPI) >> 2;        // BN / 4 of the tile's columns
-        int slot = 0;
-        uint32_t slot_phase = 0;
-        bool ok = true;
-        for (int64_t item = first_item; ok && item < total; item += item_step) {
-            const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
-            const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
-            float acc[R::COLS];
+    }
+    // ---------------------------------------------------------------- epilogue
+    constexpr int W = R::COLS < 16 ? 8 : 16;                 // columns of a load: the running sums and these stay within the registers
+    const int q = warp & 3;                                  // lane quarter of the tensor memory
+    const int part = (warp - P16_FIRST_EPI) >> 2;            // BN / 4 of the tile's columns
+    float acc[R::COLS];
+    // the tile's sums (of the member's blocks)
+    int slot = 0;
+    uint32_t slot_phase = 0;
+    auto collect = [&](const Tile16 &t) {
+        const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
 #pragma unroll
-            for (int c = 0; c < R::COLS; ++c) acc[c] = 0.0f;
-            for (int kb0 = 0; ok && kb0 < blocks; kb0 += p.core.seg) {
-                ok = wait(tfull_bar + 8 * slot, (slot_phase >> slot) & 1u);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(slot * BN + part * R::COLS);
+        for (int c = 0; c < R::COLS; ++c) acc[c] = 0.0f;
+        for (int kb0 = first_block(blocks), end = end_block(blocks); kb0 < end; kb0 += p.core.seg) {
+            if (!wait(tfull_bar + 8 * slot, (slot_phase >> slot) & 1u)) return false;
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + static_cast<uint32_t>(slot * BN + part * R::COLS);
 #pragma unroll
-                for (int c0 = 0; c0 < R::COLS; c0 += W) {
-                    if (part * R::COLS + c0 >= t.cols) break;
-                    uint32_t v[W];
-                    if constexpr (W == 16) tmem_ld16(taddr + c0, v);
-                    else tmem_ld8(taddr + c0, v);
+            for (int c0 = 0; c0 < R::COLS; c0 += W) {
+                if (part * R::COLS + c0 >= t.cols) break;
+                uint32_t v[W];
+                if constexpr (W == 16) tmem_ld16(taddr + c0, v);
+                else tmem_ld8(taddr + c0, v);
 #pragma unroll
-                    for (int c = 0; c < W; ++c) acc[c0 + c] += __uint_as_float(v[c]);
-                }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (CG == 1) mbar_arrive_relaxed(tempty_bar + 8 * slot);
-                    else mbar_arrive_cluster_relaxed(map_to_cta(tempty_bar + 8 * slot, 0));
-                }
-                slot_phase ^= 1u << slot;
-                slot ^= 1;
+                for (int c = 0; c < W; ++c) acc[c0 + c] += __uint_as_float(v[c]);
             }
-            if (!ok) break;
-            P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 1) mbar_arrive_relaxed(tempty_bar + 8 * slot);
+                else mbar_arrive_cluster_relaxed(map_to_cta(tempty_bar + 8 * slot, pair));
+            }
+            slot_phase ^= 1u << slot;
+            slot ^= 1;
+        }
+        return true;
+    };
+    if constexpr (SPLIT == 1) {
+        if (warp >= P16_FIRST_EPI)
+            for (int64_t item = first_item; item < total; item += item_step) {
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                if (!collect(t)) break;
+                P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS);
+            }
+    } else {
+        constexpr int OWN = R::COLS / SPLIT;
+        const bool works = warp >= P16_FIRST_EPI && first_item < total;
+        typename P::Tile t;
+        bool ok = works;
+        if (works) {
+            t = P::template decode<CG, BN>(p, table, first_item);
+            ok = collect(t);
+        }
+        // box of a warp and a sender: [column][lane]
+        const uint32_t box = ring + static_cast<uint32_t>((warp - P16_FIRST_EPI) * SPLIT * OWN * 128 + lane * 4);
+        __syncwarp();
+        cluster_sync_all();                                  // every member's products are done: its ring is free
+        if (ok) {
+#pragma unroll
+            for (int o = 0; o < SPLIT; ++o)
+                if (o != member) {
+                    const uint32_t to = map_to_cta(box + static_cast<uint32_t>(member * OWN * 128), static_cast<uint32_t>(o * CG) + rank);
+#pragma unroll
+                    for (int c = 0; c < OWN; ++c) store_cluster(to + c * 128, acc[o * OWN + c]);
+                }
+        }
+        __syncwarp();
+        cluster_sync_all();
+        if (ok) {
+            float own[OWN], sum[OWN];
+#pragma unroll
+            for (int c = 0; c < OWN; ++c) {
+                own[c] = acc[c];
+#pragma unroll
+                for (int o = 1; o < SPLIT; ++o) own[c] = o == member ? acc[o * OWN + c] : own[c];
+                sum[c] = 0.0f;
+            }
+            const float *from = reinterpret_cast<const float *>(smem_raw + (box - raw));
+#pragma unroll
+            for (int o = 0; o < SPLIT; ++o)
+#pragma unroll
+                for (int c = 0; c < OWN; ++c) sum[c] += o == member ? own[c] : from[(o * OWN + c) * 32];
+            P::template store<CG, BN>(p, t, sum, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS + member * OWN);
         }
     }
 
     tc_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync_all();          // neither CTA leaves while the other may still touch it
+    if (CG * SPLIT > 1) cluster_sync_all();   // no CTA leaves while another may still touch it
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc<CG>(tmem_base, TMEM_COLUMNS);
@@ -373,24 +460,38 @@ inline bool make_map16(CUtensorMap *map, bool bf16, const void *base, int64_t in
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <class P, int CG, int BN, int PLANES>
+// Matrices in plane pairs: [matrix][line][chunk of 64 elements][hi, lo][64], box = 64 elements of one plane x 64 lines
+inline bool make_pair_map16(CUtensorMap *map, const void *base, int64_t chunks, int64_t lines, int64_t matrices)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {64, static_cast<cuuint64_t>(2 * chunks), static_cast<cuuint64_t>(lines), static_cast<cuuint64_t>(matrices)};
+    cuuint64_t strides[3] = {128, static_cast<cuuint64_t>(256 * chunks), static_cast<cuuint64_t>(256 * chunks * lines)};
+    cuuint32_t box[4] = {64, 1, 64, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class P, int CG, int BN, int PLANES, int SPLIT>
 oz_status_t launch_product16(const CUtensorMap &mapA, const CUtensorMap &mapB, const typename P::Params &p, int64_t most_tiles,
                              size_t table_bytes, cudaStream_t stream)
 {
-    auto kernel = product16_kernel<P, CG, BN, PLANES>;
+    auto kernel = product16_kernel<P, CG, BN, PLANES, SPLIT>;
     static std::atomic<unsigned long long> ready{0};
     // (one request for the largest table: the shared memory that a kernel may take is set once a device)
     OZ_CUDA_CHECK(allow_shared(kernel, kMaxShared, ready));
+    // persistent CTAs; a cluster that shares its tile has one tile only
     int64_t groups = sm_count() / CG;
-    if (most_tiles < groups) groups = most_tiles;
+    if (SPLIT > 1 || most_tiles < groups) groups = most_tiles;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(groups * CG));
+    cfg.gridDim = dim3(static_cast<unsigned>(groups * CG * SPLIT));
     cfg.blockDim = dim3(P16_THREADS);
     cfg.dynamicSmemBytes = P16_RING_BYTES + 1024 + P16_BARRIER_BYTES + table_bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CG;
+    attr[0].val.clusterDim.x = CG * SPLIT;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
