@@ -31,6 +31,7 @@ struct GroupedParams {
     int64_t ldc, strideC;
     int ctype, accumulate;
     int shared_a;                   // one A for all groups
+    int a_mn;                       // A along its rows
     unsigned int *status;
     Core16 core;
 };
@@ -237,7 +238,17 @@ struct GroupedPolicy {
         int rows, valid;            // rows of C from the tile's first on, columns that belong to the group
         int64_t c;                  // element of C at the tile's first row and column
     };
-    static constexpr bool RAGGED_K = INNER;
+    struct Maps {
+        CUtensorMap a, b;
+    };
+    static constexpr bool RAGGED_K = INNER, COOPERATIVE = false;
+    static __device__ __forceinline__ const CUtensorMap *map_a(const Maps &m, int) { return &m.a; }
+    static __device__ __forceinline__ const CUtensorMap *map_b(const Maps &m, int) { return &m.b; }
+    static __device__ __forceinline__ int phases(const Params &) { return 1; }
+    static __device__ __forceinline__ bool ready(const Params &, int, volatile int *) { return true; }
+    static __device__ __forceinline__ void done(const Params &, int) {}
+    static __device__ __forceinline__ int a_mn(const Params &p, const Tile &, int) { return INNER ? 1 : p.a_mn; }
+    static __device__ __forceinline__ int b_mn(const Params &, const Tile &, int) { return INNER ? 1 : 0; }
 
     static __device__ __forceinline__ void setup(const Params &p, int width, int *table)
     {
@@ -245,7 +256,7 @@ struct GroupedPolicy {
     }
 
     template <int CG, int BN>
-    static __device__ __forceinline__ int64_t total(const Params &p, const int *table)
+    static __device__ __forceinline__ int64_t total(const Params &p, const int *table, int)
     {
         const uint32_t tiles_m = static_cast<uint32_t>((p.m + 128 * CG - 1) / (128 * CG));
         if (INNER) return static_cast<int64_t>(p.groups) * tiles_m * static_cast<uint32_t>((p.n + BN - 1) / BN);
@@ -254,7 +265,7 @@ struct GroupedPolicy {
 
     // (the host sends launches of 2^31 tiles and more elsewhere: 32-bit divisions are enough)
     template <int CG, int BN>
-    static __device__ __forceinline__ Tile decode(const Params &p, const int *table, int64_t item64)
+    static __device__ __forceinline__ Tile decode(const Params &p, const int *table, int, int64_t item64)
     {
         const uint32_t item = static_cast<uint32_t>(item64), tiles_m = static_cast<uint32_t>((p.m + 128 * CG - 1) / (128 * CG));
         Tile t;
@@ -302,10 +313,10 @@ struct GroupedPolicy {
 };
 
 template <bool INNER, int CG, int BN, int SPLIT = 1>
-oz_status_t launch_tiles(GroupedParams &p, bool bf16, const CUtensorMap &mapA, const CUtensorMap &mapB, int64_t most, cudaStream_t stream)
+oz_status_t launch_tiles(GroupedParams &p, bool bf16, const typename GroupedPolicy<INNER>::Maps &maps, int64_t most, cudaStream_t stream)
 {
-    p.core.idesc = idesc16(bf16, p.core.a_mn, p.core.b_mn, CG);
-    return launch_product16<GroupedPolicy<INNER>, CG, BN, 1, SPLIT>(mapA, mapB, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
+    p.core.idesc = idesc16(bf16, CG);
+    return launch_product16<GroupedPolicy<INNER>, CG, BN, 1, SPLIT>(maps, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
 }
 
 // tiles of 128 cg x bn at most: what the host knows of the groups is their number and that of all columns
@@ -329,8 +340,7 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
     if (reinterpret_cast<uintptr_t>(p.A) % 16 || reinterpret_cast<uintptr_t>(p.B) % 16 || lda % 8 || ldb % 8 || (!p.shared_a && p.strideA % 8))
         return OZ_OK;
     const bool bf16 = type == OZ_BF16;
-    p.core.a_mn = p.rowA == 1 && p.innerA != 1;
-    p.core.b_mn = INNER;
+    p.a_mn = p.rowA == 1 && p.innerA != 1;
     p.core.status = p.status;
     // sums that become 16-bit numbers need no segments
     p.core.seg = p.ctype == OZ_F32 ? 4 : 1 << 24;
@@ -338,18 +348,18 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
     const int64_t mean = INNER ? p.n : p.n / p.groups;
     const bool pairs = INNER || mean > 64;
     const int bn = pairs ? 256 : mean > 32 ? 64 : 32;
-    CUtensorMap mapA, mapB;
+    typename GroupedPolicy<INNER>::Maps maps;
     const int64_t za = p.shared_a ? 1 : p.groups;
     const int boxB = bn == 32 ? 32 : 64;
-    if (!(p.core.a_mn ? make_map16(&mapA, bf16, p.A, p.m, inner, lda, za, za > 1 ? p.strideA : lda, 64)
-                      : make_map16(&mapA, bf16, p.A, inner, p.m, lda, za, za > 1 ? p.strideA : lda, 64)) ||
-        !(INNER ? make_map16(&mapB, bf16, p.B, p.n, inner, ldb, 1, ldb, boxB) : make_map16(&mapB, bf16, p.B, inner, p.n, ldb, 1, ldb, boxB)))
+    if (!(p.a_mn ? make_map16(&maps.a, bf16, p.A, p.m, inner, lda, za, za > 1 ? p.strideA : lda, 64)
+                      : make_map16(&maps.a, bf16, p.A, inner, p.m, lda, za, za > 1 ? p.strideA : lda, 64)) ||
+        !(INNER ? make_map16(&maps.b, bf16, p.B, p.n, inner, ldb, 1, ldb, boxB) : make_map16(&maps.b, bf16, p.B, inner, p.n, ldb, 1, ldb, boxB)))
         return OZ_OK;
     *taken = true;
-    if (pairs) return launch_tiles<INNER, 2, 256>(p, bf16, mapA, mapB, most_tiles<INNER>(p, 2, 256), stream);
+    if (pairs) return launch_tiles<INNER, 2, 256>(p, bf16, maps, most_tiles<INNER>(p, 2, 256), stream);
     if constexpr (!INNER) {
-        if (bn == 64) return launch_tiles<INNER, 1, 64>(p, bf16, mapA, mapB, most_tiles<INNER>(p, 1, 64), stream);
-        return launch_tiles<INNER, 1, 32>(p, bf16, mapA, mapB, most_tiles<INNER>(p, 1, 32), stream);
+        if (bn == 64) return launch_tiles<INNER, 1, 64>(p, bf16, maps, most_tiles<INNER>(p, 1, 64), stream);
+        return launch_tiles<INNER, 1, 32>(p, bf16, maps, most_tiles<INNER>(p, 1, 32), stream);
     }
     return OZ_OK;
 }

@@ -12,11 +12,10 @@
 // Planes in memory: [matrix][line][chunk of 64 elements][hi, lo][64], so that both halves of an element lie at a fixed distance, and a block
 // of an operand is the same box whether its lines or its elements are the inner dimension.  Elements behind the last are zero.
 //
-// S and P are symmetric: only tiles on and below the diagonal are computed, those below are stored twice.  (Tiles on it are stored
-// as computed.)  X keeps its r rows consecutive: for X X^T it is an operand stored along its rows, for P X one stored along the inner dimension,
-// both by the same bulk copies, and S and P are read along whichever direction suits.
+// X keeps its r rows consecutive: for X X^T it is an operand stored along its rows, for P X one stored along the inner dimension,
+// both by the same bulk copies.  S and P are symmetric and computed on and below the diagonal only (see NewtonPolicy).
 //
-// Launches: sum of squares, planes of X, then three products a step.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
+// Launches: sum of squares, planes of X, all products.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
 // three times that on the pipe.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -34,6 +33,7 @@ constexpr int kMaxSteps = 100;
 constexpr int NORM_THREADS = 256;
 constexpr int MAX_PARTS = 64;                      // partial sums of squares of a matrix
 constexpr int PLANE_TILE = 64;
+constexpr unsigned long long kPhaseLimitNs = 4000000000ull;        // wait for the other blocks
 
 __device__ __forceinline__ float load_number(const void *X, int64_t at, int type)
 {
@@ -70,6 +70,7 @@ struct MatrixParams {
     int r, c, ld;                   // X is r x c, r <= c, its columns ld half-precision numbers apart
     int parts;
     double *sums;                   // [count][parts]
+    unsigned int *arrived;          // set to zero
     double eps;
     float scale;                    // of the planes
     __half *X;                      // plane pairs: [count][c][ld]
@@ -98,6 +99,7 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const MatrixParams p
     if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
+        if (blockIdx.x == 0) *p.arrived = 0u;
         for (int w = 1; w < NORM_THREADS / 32; ++w) sum += warp_sums[w];
         p.sums[blockIdx.x] = sum;
     }
@@ -162,202 +164,261 @@ __global__ void __launch_bounds__(256) planes_kernel(const MatrixParams p)
 }
 
 // ---------------------------------------------------------------- products
-enum { kGram, kPolynomial, kApply, kApplyLast };
+enum { kGram, kPolynomial, kApply };
 
 struct NewtonParams {
-    int count, r, c, ld;
-    float alpha, beta;              // result = alpha accumulator + beta old
-    const __half *old;              // plane pairs [count][r or c][ld]: S of kPolynomial, X of kApply
-    __half *out;                    // plane pairs
-    void *O;                        // kApplyLast
+    int count, r, c, ld, steps;
+    __half *x[2], *gram, *poly;     // plane pairs [count][c or r][ld]
+    void *O;
     int64_t ldo, strideO;
     int otype, transposed;
+    unsigned int *arrived;          // blocks that have finished a phase, all phases together
     Core16 core;
+    float alpha[3 * kMaxSteps], beta[3 * kMaxSteps];      // of each phase: result = alpha accumulator + beta old
 };
 
-template <int MODE>
+// All steps in one launch: phase 3 s is S = X X^T of step s, 3 s + 1 P, 3 s + 2 the new X.  The blocks meet between the phases.
+// Tiles are 256 rows x BN columns by pairs: the three plane products of a block read shared memory at 106 bytes a cycle with BN = 256; those of
+// tiles of 128 x 128 by single CTAs would at 213 of the 128 that it has.
+// Of S and P only blocks of 256 x 256 on and below the diagonal are computed and stored, line j holding elements i >= j (and all of the
+// diagonal block).  A product that wants a block above takes the one below with its directions exchanged: an operand stored along its rows
+// instead of along the inner dimension, which the tensor core reads as well.
 struct NewtonPolicy {
     using Params = NewtonParams;
-    struct Tile : Tile16 {
-        int matrix, j0;
-        bool mirror;
+    struct Maps {
+        CUtensorMap x[2], gram, poly;
     };
-    static constexpr bool RAGGED_K = false, SYMMETRIC = MODE == kGram || MODE == kPolynomial;
+    struct Tile : Tile16 {
+        int matrix, phase;
+    };
+    static constexpr bool RAGGED_K = false, COOPERATIVE = true;
 
+    static __device__ __forceinline__ const CUtensorMap *map_a(const Maps &m, int phase)
+    {
+        return phase % 3 == kGram ? &m.x[phase / 3 & 1] : phase % 3 == kPolynomial ? &m.gram : &m.poly;
+    }
+    static __device__ __forceinline__ const CUtensorMap *map_b(const Maps &m, int phase)
+    {
+        return phase % 3 == kPolynomial ? &m.gram : &m.x[phase / 3 & 1];
+    }
     static __device__ __forceinline__ void setup(const Params &, int, int *) {}
+    static __device__ __forceinline__ int phases(const Params &p) { return 3 * p.steps; }
 
-    template <int CG, int BN>
-    static __device__ __forceinline__ uint32_t tiles_each(const Params &p)
+    // Blocks arrive with a release after all their stores, and whoever goes on acquires; the fences carry the stores over to the bulk copies.
+    static __device__ __forceinline__ bool ready(const Params &p, int phase, volatile int *abort_flag)
     {
-        const uint32_t tm = static_cast<uint32_t>((p.r + 128 * CG - 1) / (128 * CG));
-        static_assert(!SYMMETRIC || 128 * CG == BN, "square tiles");
-        return SYMMETRIC ? tm * (tm + 1) / 2 : tm * static_cast<uint32_t>((p.c + BN - 1) / BN);
+        if (phase == 0) return true;
+        const unsigned int want = static_cast<unsigned int>(phase) * gridDim.x;
+        unsigned long long start = 0;
+        for (unsigned int poll = 0;; ++poll) {
+            unsigned int have;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(p.arrived) : "memory");
+            if (__all_sync(0xFFFFFFFFu, have >= want)) break;
+            if (*abort_flag) return false;
+            if (poll % 256 == 255) {
+                const unsigned long long now = global_timer_ns();
+                if (start == 0) start = now;
+                if (__any_sync(0xFFFFFFFFu, now - start > kPhaseLimitNs)) {
+                    *abort_flag = 1;
+                    atomicOr(p.core.status, 1u << OZ_ERR_TIMEOUT);
+                    return false;
+                }
+            }
+        }
+        asm volatile("fence.proxy.async;" ::: "memory");
+        return true;
+    }
+    static __device__ __forceinline__ void done(const Params &p, int)
+    {
+        __threadfence();
+        asm volatile("fence.proxy.async;" ::: "memory");
+        asm volatile("bar.sync 1, %0;" ::"n"(P16_EPI_WARPS * 32) : "memory");
+        if (threadIdx.x == 32 * P16_FIRST_EPI) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.arrived) : "memory");
+    }
+
+    // tiles of a matrix: all of X, or those of S and P that touch the lower blocks of 256
+    template <int BN>
+    static __host__ __device__ __forceinline__ uint32_t tiles_each(int r, int c, int phase)
+    {
+        const uint32_t tm = static_cast<uint32_t>((r + 255) / 256), wide = 256 / BN;
+        if (phase % 3 == kApply) return tm * static_cast<uint32_t>((c + BN - 1) / BN);
+        const uint32_t last = (static_cast<uint32_t>(r) - 256 * (tm - 1) + BN - 1) / BN;          // columns of tiles of the last block
+        return wide * tm * (tm - 1) / 2 + (tm - 1) * wide + last;
+    }
+    template <int CG, int BN>
+    static __device__ __forceinline__ int64_t total(const Params &p, const int *, int phase)
+    {
+        return static_cast<int64_t>(p.count) * tiles_each<BN>(p.r, p.c, phase);
     }
 
     template <int CG, int BN>
-    static __device__ __forceinline__ int64_t total(const Params &p, const int *)
+    static __device__ __forceinline__ Tile decode(const Params &p, const int *, int phase, int64_t item)
     {
-        return static_cast<int64_t>(p.count) * tiles_each<CG, BN>(p);
-    }
-
-    template <int CG, int BN>
-    static __device__ __forceinline__ Tile decode(const Params &p, const int *, int64_t item)
-    {
-        const uint32_t each = tiles_each<CG, BN>(p);
+        const uint32_t each = tiles_each<BN>(p.r, p.c, phase);
         Tile t;
+        t.phase = phase;
         t.matrix = static_cast<int>(static_cast<uint32_t>(item) / each);
         const uint32_t in = static_cast<uint32_t>(item) - static_cast<uint32_t>(t.matrix) * each;
         uint32_t ti, tj;
-        if (SYMMETRIC) {
-            ti = static_cast<uint32_t>((sqrtf(8.0f * static_cast<float>(in) + 1.0f) - 1.0f) * 0.5f);
-            while (ti * (ti + 1) / 2 > in) --ti;
-            while ((ti + 1) * (ti + 2) / 2 <= in) ++ti;
-            tj = in - ti * (ti + 1) / 2;
-        } else {
-            const uint32_t tm = static_cast<uint32_t>((p.r + 128 * CG - 1) / (128 * CG));
+        if (phase % 3 == kApply) {
+            const uint32_t tm = static_cast<uint32_t>((p.r + 255) / 256);
             ti = in % tm;
             tj = in / tm;
+        } else {
+            // block row ti has wide (ti + 1) tiles
+            constexpr uint32_t wide = 256 / BN;
+            const uint32_t block = in / wide;
+            ti = static_cast<uint32_t>((sqrtf(8.0f * static_cast<float>(block) + 1.0f) - 1.0f) * 0.5f);
+            while (ti * (ti + 1) / 2 > block) --ti;
+            while ((ti + 1) * (ti + 2) / 2 <= block) ++ti;
+            tj = in - wide * (ti * (ti + 1) / 2);
         }
-        t.mirror = SYMMETRIC && ti != tj;
-        t.a_row = static_cast<int>(ti) * 128 * CG;
-        t.b_row = t.j0 = static_cast<int>(tj) * BN;
+        t.a_row = static_cast<int>(ti) * 256;
+        t.b_row = static_cast<int>(tj) * BN;
         t.a_z = t.b_z = t.matrix;
         t.k_begin = 0;
-        t.k_len = MODE == kGram ? p.c : p.r;
-        const int left = (SYMMETRIC ? p.r : p.c) - t.j0;
-        // (an operand along its rows comes in whole chunks: half of the columns from each CTA)
-        constexpr int GRAIN = MODE == kGram ? 64 * CG : 16 * CG;
-        t.cols = left >= BN ? BN : (left + GRAIN - 1) / GRAIN * GRAIN;
+        t.k_len = phase % 3 == kGram ? p.c : p.r;
+        const int left = (phase % 3 == kApply ? p.c : p.r) - t.b_row;
+        t.cols = BN > 128 && left <= 128 ? 128 : BN;
         return t;
     }
 
-    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and N columns, eight at a time at most.
+    static __device__ __forceinline__ int a_mn(const Params &, const Tile &t, int block)
+    {
+        return t.phase % 3 == kGram || block >> 2 <= t.a_row >> 8;
+    }
+    static __device__ __forceinline__ int b_mn(const Params &, const Tile &t, int block)
+    {
+        return t.phase % 3 == kGram || (t.phase % 3 == kPolynomial && block >> 2 < t.b_row >> 8);
+    }
+
+    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and N columns, eight at a time.
     template <int CG, int BN, int N>
     static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col)
     {
-        const int i = t.a_row + row, j0 = t.j0 + col, lines = SYMMETRIC ? p.r : p.c, left = lines - j0;
-        if (i >= (MODE == kApplyLast ? p.r : p.ld / 2) || left <= 0) return;
-        if (left >= N) store_columns<true>(p, t, acc, i, j0, lines, left);
-        else store_columns<false>(p, t, acc, i, j0, lines, left);
-    }
-
-    template <bool FULL, int N>
-    static __device__ __forceinline__ void store_columns(const Params &p, const Tile &t, const float (&acc)[N], int i, int j0, int lines, int left)
-    {
-        constexpr int STEP = N < 8 ? N : 8;
-        const int64_t base = static_cast<int64_t>(t.matrix) * lines * p.ld, at = base + static_cast<int64_t>(j0) * p.ld + pair_at(i);
-        const __half *old = MODE == kGram ? nullptr : p.old + at;
-        // some results: alpha accumulator + beta old
-        auto results = [&](float (&v)[STEP], int c0) {
-            __half hi[STEP], lo[STEP];
-            if constexpr (MODE != kGram) {
-#pragma unroll
-                for (int c = 0; c < STEP; ++c) {
-                    const bool inside = FULL || c0 + c < left;
-                    hi[c] = inside ? old[0] : __half();
-                    lo[c] = inside ? old[64] : __half();
-                    old += p.ld;
-                }
-            }
-#pragma unroll
-            for (int c = 0; c < STEP; ++c) {
-                v[c] = p.alpha * acc[c0 + c];
-                if constexpr (MODE != kGram) v[c] = fmaf(p.beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
-            }
-        };
-        if constexpr (MODE == kApplyLast) {
+        const int i = t.a_row + row, j0 = t.b_row + col, lines = t.phase % 3 == kApply ? p.c : p.r, left = lines - j0;
+        const bool last = t.phase == 3 * p.steps - 1;
+        if (i >= (last ? p.r : p.ld / 2) || left <= 0) return;
+        const float alpha = p.alpha[t.phase], beta = p.beta[t.phase];
+        const int64_t at = (static_cast<int64_t>(t.matrix) * lines + j0) * p.ld + pair_at(i);
+        const int from = t.phase / 3 & 1;
+        if (last) {
+            const __half *old = p.x[from] + at;
             auto as = [&](auto *O) {
-                using T = typename std::remove_pointer<decltype(O)>::type;
                 O += t.matrix * p.strideO;
                 if (p.transposed) {
-                    // the row's elements are consecutive
-                    constexpr int WIDE = STEP * static_cast<int>(sizeof(T)) / 16;
-                    T *to = O + j0 + i * p.ldo;
-                    const bool wide = FULL && reinterpret_cast<uintptr_t>(to) % 16 == 0;
-#pragma unroll
-                    for (int c0 = 0; c0 < N; c0 += STEP) {
-                        float v[STEP];
-                        results(v, c0);
-                        __align__(16) T w[STEP];
-#pragma unroll
-                        for (int c = 0; c < STEP; ++c) w[c] = from_float<T>(v[c]);
-                        if (WIDE > 0 && wide) {
-#pragma unroll
-                            for (int c = 0; c < WIDE; ++c) reinterpret_cast<uint4 *>(to + c0)[c] = reinterpret_cast<const uint4 *>(w)[c];
-                        } else {
-#pragma unroll
-                            for (int c = 0; c < STEP; ++c)
-                                if (FULL || c0 + c < left) to[c0 + c] = w[c];
-                        }
-                    }
+                    if (left >= N) store_last<true, true>(p, old, O + j0 + i * p.ldo, acc, alpha, beta, left);
+                    else store_last<false, true>(p, old, O + j0 + i * p.ldo, acc, alpha, beta, left);
                 } else {
-                    T *to = O + i + j0 * p.ldo;
-#pragma unroll
-                    for (int c0 = 0; c0 < N; c0 += STEP) {
-                        float v[STEP];
-                        results(v, c0);
-#pragma unroll
-                        for (int c = 0; c < STEP; ++c) {
-                            if (FULL || c0 + c < left) *to = from_float<T>(v[c]);
-                            to += p.ldo;
-                        }
-                    }
+                    if (left >= N) store_last<true, false>(p, old, O + i + j0 * p.ldo, acc, alpha, beta, left);
+                    else store_last<false, false>(p, old, O + i + j0 * p.ldo, acc, alpha, beta, left);
                 }
             };
             if (p.otype == OZ_F32) as(static_cast<float *>(p.O));
             else if (p.otype == OZ_BF16) as(static_cast<__nv_bfloat16 *>(p.O));
             else as(static_cast<__half *>(p.O));
+        } else if (t.phase % 3 == kGram) {
+            if (left >= N) store_planes<true, false>(p, nullptr, p.gram + at, acc, alpha, beta, left);
+            else store_planes<false, false>(p, nullptr, p.gram + at, acc, alpha, beta, left);
         } else {
-            __half *to = p.out + at;
-            // The same elements of the other triangle: elements j0 .. of line i, where that is one.  Behind the last column they are the zeros that
-            // belong there.
-            __half *mirror = p.out + base + static_cast<int64_t>(i) * p.ld + pair_at(j0);
-            const bool mirrored = SYMMETRIC && t.mirror && i < lines;
+            const __half *old = (t.phase % 3 == kPolynomial ? p.gram : p.x[from]) + at;
+            __half *to = (t.phase % 3 == kPolynomial ? p.poly : p.x[from ^ 1]) + at;
+            if (left >= N) store_planes<true, true>(p, old, to, acc, alpha, beta, left);
+            else store_planes<false, true>(p, old, to, acc, alpha, beta, left);
+        }
+    }
+
+    // v = alpha acc + beta old of columns c0 .. c0 + 7; `old` moves on.  (Written by other blocks in this launch: from L2.)
+    template <bool FULL, bool OLD, int N>
+    static __device__ __forceinline__ void results(float (&v)[8], const __half *&old, int64_t ld, const float (&acc)[N], int c0, float alpha,
+                                                   float beta, int left)
+    {
+        __half hi[8], lo[8];
+        if constexpr (OLD) {
 #pragma unroll
-            for (int c0 = 0; c0 < N; c0 += STEP) {
-                float v[STEP];
-                __align__(16) __half hi[STEP], lo[STEP];
-                results(v, c0);
+            for (int c = 0; c < 8; ++c) {
+                const bool inside = FULL || c0 + c < left;
+                hi[c] = inside ? __ldcg(old) : __half();
+                lo[c] = inside ? __ldcg(old + 64) : __half();
+                old += ld;
+            }
+        }
 #pragma unroll
-                for (int c = 0; c < STEP; ++c) split_planes(v[c], &hi[c], &lo[c]);
+        for (int c = 0; c < 8; ++c) {
+            v[c] = alpha * acc[c0 + c];
+            if constexpr (OLD) v[c] = fmaf(beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
+        }
+    }
+
+    template <bool FULL, bool OLD, int N>
+    static __device__ __forceinline__ void store_planes(const Params &p, const __half *old, __half *to, const float (&acc)[N], float alpha, float beta, int left)
+    {
+        static_assert(N % 8 == 0, "columns eight at a time");
 #pragma unroll
-                for (int c = 0; c < STEP; ++c) {
-                    if (FULL || c0 + c < left) {
-                        to[0] = hi[c];
-                        to[64] = lo[c];
-                    }
-                    to += p.ld;
-                }
-                static_assert(!SYMMETRIC || STEP == 8, "whole vectors");
-                if (mirrored && (FULL || c0 < left)) {
-                    *reinterpret_cast<uint4 *>(mirror + c0) = *reinterpret_cast<const uint4 *>(hi);
-                    *reinterpret_cast<uint4 *>(mirror + c0 + 64) = *reinterpret_cast<const uint4 *>(lo);
-                }
+        for (int c0 = 0; c0 < N; c0 += 8) {
+            float v[8];
+            results<FULL, OLD>(v, old, p.ld, acc, c0, alpha, beta, left);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                if (FULL || c0 + c < left) split_planes(v[c], to, to + 64);
+                to += p.ld;
+            }
+        }
+    }
+
+    // the result itself: down its columns, or, transposed, the row's consecutive elements
+    template <bool FULL, bool TRANSPOSED, int N, class T>
+    static __device__ __forceinline__ void store_last(const Params &p, const __half *old, T *to, const float (&acc)[N], float alpha, float beta, int left)
+    {
+        const bool wide = TRANSPOSED && FULL && reinterpret_cast<uintptr_t>(to) % 16 == 0;
+#pragma unroll
+        for (int c0 = 0; c0 < N; c0 += 8) {
+            float v[8];
+            results<FULL, true>(v, old, p.ld, acc, c0, alpha, beta, left);
+            __align__(16) T w[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) w[c] = from_float<T>(v[c]);
+            if (wide) {
+#pragma unroll
+                for (int c = 0; c < static_cast<int>(sizeof(T)) / 2; ++c) reinterpret_cast<uint4 *>(to + c0)[c] = reinterpret_cast<const uint4 *>(w)[c];
+            } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (FULL || c0 + c < left) to[TRANSPOSED ? c0 + c : (c0 + c) * p.ldo] = w[c];
             }
         }
     }
 };
 
-template <int MODE>
-oz_status_t launch_newton(NewtonParams &p, const CUtensorMap &mapA, const CUtensorMap &mapB, cudaStream_t stream)
+template <int BN>
+oz_status_t launch_newton(const NewtonPolicy::Maps &maps, const NewtonParams &p, cudaStream_t stream)
 {
-    constexpr bool SYMMETRIC = NewtonPolicy<MODE>::SYMMETRIC;
-    const int64_t tm = (p.r + 255) / 256, tiles = p.count * (SYMMETRIC ? tm * (tm + 1) / 2 : tm * ((p.c + 255) / 256));
-    p.core.a_mn = p.core.b_mn = MODE == kGram;
-    p.core.idesc = idesc16(false, p.core.a_mn, p.core.b_mn, 2);
-    // Tiles are always 256 x 256 by pairs: the three plane products of a block read shared memory at 106 bytes a cycle; those of tiles of 128 x 128 by
-    // single CTAs would at 213 of the 128 that it has.  Few tiles are shared out along the inner dimension.
-    const int64_t pairs = sm_count() / 2;
-    if (4 * tiles <= pairs) return launch_product16<NewtonPolicy<MODE>, 2, 256, 2, 4>(mapA, mapB, p, tiles, 0, stream);
-    if (2 * tiles <= pairs) return launch_product16<NewtonPolicy<MODE>, 2, 256, 2, 2>(mapA, mapB, p, tiles, 0, stream);
-    return launch_product16<NewtonPolicy<MODE>, 2, 256, 2, 1>(mapA, mapB, p, tiles, 0, stream);
+    int64_t most = 0;
+    for (int phase = 0; phase < 3; ++phase) {
+        const int64_t tiles = static_cast<int64_t>(p.count) * NewtonPolicy::tiles_each<BN>(p.r, p.c, phase);
+        if (tiles > most) most = tiles;
+    }
+    if (most >= (1ll << 31)) return OZ_ERR_UNSUPPORTED;
+    return launch_product16<NewtonPolicy, 2, BN, 2, 1>(maps, p, most, 0, stream);
+}
+
+// cycles of a step with tiles of 256 x BN: rounds over the pairs, blocks of 64 inner indices at `each` cycles
+template <int BN>
+int64_t step_cycles(const NewtonParams &p, int each)
+{
+    int64_t sum = 0;
+    for (int phase = 0; phase < 3; ++phase) {
+        const int64_t tiles = static_cast<int64_t>(p.count) * NewtonPolicy::tiles_each<BN>(p.r, p.c, phase), pairs = sm_count() / 2;
+        sum += (tiles + pairs - 1) / pairs * (((phase == kGram ? p.c : p.r) + 63) / 64 * each);
+    }
+    return sum;
 }
 
 // ---------------------------------------------------------------- host side
 struct Layout {
     int64_t r, c, chunks;
     int parts;
-    size_t sums, x[2], s, poly, total;
+    size_t arrived, sums, x[2], s, poly, total;
 };
 
 Layout layout_of(int64_t m, int64_t n, int64_t count)
@@ -374,6 +435,7 @@ Layout layout_of(int64_t m, int64_t n, int64_t count)
         at += static_cast<size_t>(round_up(bytes, 256));
         return here;
     };
+    l.arrived = take(4);
     l.sums = take(count * l.parts * 8);
     l.x[0] = take(count * l.c * l.chunks * 256);
     l.x[1] = take(count * l.c * l.chunks * 256);
@@ -470,9 +532,9 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     char *ws = static_cast<char *>(workspace);
     __half *x[2] = {reinterpret_cast<__half *>(ws + l.x[0]), reinterpret_cast<__half *>(ws + l.x[1])};
     __half *gram = reinterpret_cast<__half *>(ws + l.s), *poly = reinterpret_cast<__half *>(ws + l.poly);
-    CUtensorMap map_x[2], map_s, map_p;
-    if (steps && !(make_pair_map16(&map_x[0], x[0], l.chunks, l.c, count) && make_pair_map16(&map_x[1], x[1], l.chunks, l.c, count) &&
-                   make_pair_map16(&map_s, gram, l.chunks, l.r, count) && make_pair_map16(&map_p, poly, l.chunks, l.r, count)))
+    NewtonPolicy::Maps maps;
+    if (steps && !(make_pair_map16(&maps.x[0], x[0], l.chunks, l.c, count) && make_pair_map16(&maps.x[1], x[1], l.chunks, l.c, count) &&
+                   make_pair_map16(&maps.gram, gram, l.chunks, l.r, count) && make_pair_map16(&maps.poly, poly, l.chunks, l.r, count)))
         return OZ_ERR_CUDA;
 
     MatrixParams mp{};
@@ -493,6 +555,7 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     mp.ld = static_cast<int>(128 * l.chunks);
     mp.parts = l.parts;
     mp.sums = reinterpret_cast<double *>(ws + l.sums);
+    mp.arrived = reinterpret_cast<unsigned int *>(ws + l.arrived);
     mp.eps = eps;
     mp.scale = static_cast<float>(plane_scale(bound[0]));
     mp.X = x[0];
@@ -503,41 +566,45 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     OZ_CUDA_CHECK(launch(steps ? planes_kernel<true> : planes_kernel<false>, dim3(static_cast<unsigned>(tiles)), 256, 0, s, mp));
     count_launch(2);
 
+    if (steps == 0) return OZ_OK;
+
     NewtonParams p{};
     p.count = static_cast<int>(count);
     p.r = mp.r;
     p.c = mp.c;
     p.ld = mp.ld;
+    p.steps = steps;
+    p.x[0] = x[0];
+    p.x[1] = x[1];
+    p.gram = gram;
+    p.poly = poly;
     p.O = O;
     p.ldo = ldo;
     p.strideO = strideO;
     p.otype = otype;
     p.transposed = mp.transposed;
+    p.arrived = mp.arrived;
     // blocks of 64 an accumulator: error of the result (16 x 512 x 2048, 1024 x 1024) 0.8e-6 and 0.7e-6 with one, 1.4e-6 and 1.2e-6 with two, 5.6e-6
     // and 3.8e-6 with eight, where a rounding to 16 bits is 1.7e-3 (bfloat16) or 2e-4; the FP32 iteration in one precision has 2e-6 to 5e-6
     p.core.seg = otype == OZ_F32 ? 2 : 8;
+    p.core.idesc = idesc16(false, 2);
     p.core.status = mp.status;
     for (int step = 0; step < steps; ++step) {
         const double sx = plane_scale(bound[step]), ss = plane_scale(bound[step] * bound[step]),
-                     sp = plane_scale(largest_polynomial(b, c, bound[step] * bound[step])), next = plane_scale(bound[step + 1]);
-        const int from = step & 1;
-        p.alpha = static_cast<float>(ss / (sx * sx));
-        p.out = gram;
-        if ((st = launch_newton<kGram>(p, map_x[from], map_x[from], s)) != OZ_OK) return st;
-        p.alpha = static_cast<float>(sp * c / (ss * ss));
-        p.beta = static_cast<float>(sp * b / ss);
-        p.old = gram;
-        p.out = poly;
-        if ((st = launch_newton<kPolynomial>(p, map_s, map_s, s)) != OZ_OK) return st;
-        const bool last = step == steps - 1;
-        p.alpha = static_cast<float>((last ? 1.0 : next) / (sp * sx));
-        p.beta = static_cast<float>((last ? 1.0 : next) * a / sx);
-        p.old = x[from];
-        p.out = x[from ^ 1];
-        st = last ? launch_newton<kApplyLast>(p, map_p, map_x[from], s) : launch_newton<kApply>(p, map_p, map_x[from], s);
-        if (st != OZ_OK) return st;
+                     sp = plane_scale(largest_polynomial(b, c, bound[step] * bound[step])),
+                     next = step == steps - 1 ? 1.0 : plane_scale(bound[step + 1]);
+        float *alpha = p.alpha + 3 * step, *beta = p.beta + 3 * step;
+        alpha[kGram] = static_cast<float>(ss / (sx * sx));
+        alpha[kPolynomial] = static_cast<float>(sp * c / (ss * ss));
+        beta[kPolynomial] = static_cast<float>(sp * b / ss);
+        alpha[kApply] = static_cast<float>(next / (sp * sx));
+        beta[kApply] = static_cast<float>(next * a / sx);
     }
-    return OZ_OK;
+    // cycles of a block of 64 inner indices: the tensor cores' 1536 with 256 columns, shared memory's with fewer
+    const int64_t wide = step_cycles<256>(p, 1536), half = step_cycles<128>(p, 960), narrow = step_cycles<64>(p, 790);
+    if (wide <= half && wide <= narrow) return launch_newton<256>(maps, p, s);
+    if (half <= narrow) return launch_newton<128>(maps, p, s);
+    return launch_newton<64>(maps, p, s);
 }
 
 }  // extern "C"

@@ -48,8 +48,8 @@ template <int CG, int BN, int PLANES>
 struct Ring16 {
     static_assert(P16_EPI_WARPS * 4 * 32 * (BN / 4) <= P16_RING_BYTES, "sums of the other members of a cluster");
     static constexpr int B_ROWS = BN / CG;                                   // columns of the tile that one CTA loads
-    static constexpr int B_BOX_ROWS = B_ROWS < 64 ? B_ROWS : 64;
-    static constexpr int B_BOXES = B_ROWS / B_BOX_ROWS;
+    static constexpr int B_BOX_ROWS = B_ROWS < 64 && PLANES == 1 ? B_ROWS : 64;
+    static constexpr int B_BOXES = B_ROWS < 64 ? 1 : B_ROWS / 64;
     static constexpr int B_BOX_BYTES = B_BOX_ROWS * 128;
     static constexpr int A_PLANE = 2 * P16_BOX_BYTES;
     static constexpr int B_PLANE = B_BOXES * B_BOX_BYTES;
@@ -61,22 +61,20 @@ struct Ring16 {
 
 // what the roles need to know of a launch and of a tile, whatever the policy
 struct Core16 {
-    uint32_t idesc;             // instruction descriptor without the number of columns
-    int a_mn, b_mn;             // operand stored along its rows (MN-major)
+    uint32_t idesc;             // instruction descriptor without directions and number of columns
     int seg;                    // blocks per accumulator
     unsigned int *status;
 };
 struct Tile16 {
     int a_row, a_z, b_row, b_z; // coordinates of the tile's first row of A and column of B
     int k_begin, k_len;
-    int cols;                   // columns computed: a multiple of 16 CG
+    int cols;                   // columns computed: a multiple of 16 CG; of plane pairs, whose operand B may be along its rows, 64 or a multiple of 128
 };
 
-inline uint32_t idesc16(bool bf16, bool a_mn, bool b_mn, int cg)
+inline uint32_t idesc16(bool bf16, int cg)
 {
     const uint32_t fmt = bf16 ? 1u : 0u;
-    return (1u << 4) | (fmt << 7) | (fmt << 10) | (static_cast<uint32_t>(a_mn) << 15) | (static_cast<uint32_t>(b_mn) << 16) |
-           (static_cast<uint32_t>((128 * cg) >> 4) << 24);
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | (static_cast<uint32_t>((128 * cg) >> 4) << 24);
 }
 
 template <int CG>
@@ -145,16 +143,21 @@ __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap
 
 // Policy P:
 //   P::Params              the launch: has a Core16 `core`
+//   P::Maps                the operands' maps; P::map_a(maps, phase), P::map_b(maps, phase) point to them
 //   P::Tile                a tile: derives from Tile16
 //   P::RAGGED_K            k_begin and k_len are any numbers, and what lies behind them must not enter (MN-major operands only)
-//   P::setup(p, table)     all threads, after the predecessor's end: what `table`, shared memory of the launch's choice, holds
-//   P::total(p, table)     number of tiles
-//   P::decode<CG, BN>(p, table, item)
+//   P::setup(p, width, table)   all threads, after the predecessor's end: what `table`, shared memory of the launch's choice, holds
+//   P::phases(p)           products that follow one another in the launch, each of results of the one before
+//   P::ready(p, phase, abort_flag)   before a role's first access to what the phase before wrote; false: give up
+//   P::done(p, phase)      the epilogue warps, after their last store of a phase
+//   P::total<CG, BN>(p, table, phase)   number of tiles
+//   P::decode<CG, BN>(p, table, phase, item)
+//   P::a_mn(p, tile, block), P::b_mn(p, tile, block): whether the operand of the tile's block is stored along its rows (MN-major)
+//   P::COOPERATIVE         the launch's blocks wait for one another (between phases)
 //   P::store<CG, BN>(p, tile, acc, row, col): the thread's results, row of the tile (0 .. 128 CG - 1), as many columns from col on as acc holds
 template <class P, int CG, int BN, int PLANES, int SPLIT>
 __global__ void __launch_bounds__(P16_THREADS, 1)
-product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
-                 const __grid_constant__ typename P::Params p)
+product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_constant__ typename P::Params p)
 {
     using R = Ring16<CG, BN, PLANES>;
     constexpr int STAGES = R::STAGES;
@@ -179,8 +182,8 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        prefetch_map(&mapA);
-        prefetch_map(&mapB);
+        prefetch_map(P::map_a(maps, 0));
+        prefetch_map(P::map_b(maps, 0));
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(full_bar + 8 * s, CG);                    // a CTA's copies, or what zeroes behind them, arrive once
             mbar_init(empty_bar + 8 * s, 1);
@@ -202,7 +205,6 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
     tc_fence_after();
     dependency_release();
     const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_base_ptr, 0);
-    const int64_t total = P::template total<CG, BN>(p, table);
     unsigned int *const status = p.core.status;
     auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
     // the member's blocks of a tile
@@ -218,8 +220,12 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         bool ok = true;
         if (warp == 0) {
             // -------------------------------------------------------- copies
+            for (int ph = 0, phases = P::phases(p); ok && ph < phases; ++ph) {
+            ok = P::ready(p, ph, abort_flag);
+            const CUtensorMap *mapA = P::map_a(maps, ph), *mapB = P::map_b(maps, ph);
+            const int64_t total = P::template total<CG, BN>(p, table, ph);
             for (int64_t item = first_item; ok && item < total; item += item_step) {
-                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, ph, item);
                 const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
                 const int b_rows = t.cols / CG, b_boxes = R::B_BOXES == 1 ? 1 : (b_rows + 63) >> 6;
                 const int a_row = t.a_row + static_cast<int>(rank) * 128, b_row = t.b_row + static_cast<int>(rank) * b_rows;
@@ -239,11 +245,12 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                             bar = tail ? map_to_cta(tail_bar + 8 * stage, place) : map_to_cta(full_bar + 8 * stage, pair);
                             mbar_expect_tx_cluster(bar, bytes);
                         }
+                        const int a_mn = P::a_mn(p, t, kb), b_mn = P::b_mn(p, t, kb);
                         auto copy = [&](uint32_t dst, const CUtensorMap *map, int mn, int row, int z, int plane) {
                             const int c0 = mn ? row : kk, c1 = mn ? kk : row;
                             if constexpr (PLANES == 2) {
-                                if (CG == 1) tma_load_4d(dst, map, bar, 0, 2 * (c0 >> 6) + plane, c1, z);
-                                else tma_load_4d_pair(dst, map, bar, 0, 2 * (c0 >> 6) + plane, c1, z);
+                                if (CG == 1) tma_load_4d(dst, map, bar, c0 & 63, 2 * (c0 >> 6) + plane, c1, z);
+                                else tma_load_4d_pair(dst, map, bar, c0 & 63, 2 * (c0 >> 6) + plane, c1, z);
                             } else {
                                 if (CG == 1) tma_load_3d(dst, map, bar, c0, c1, z);
                                 else tma_load_3d_pair(dst, map, bar, c0, c1, z);
@@ -253,24 +260,25 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         for (int pl = 0; pl < PLANES; ++pl) {
 #pragma unroll
                             for (int b = 0; b < 2; ++b)
-                                copy(sa + pl * R::A_PLANE + b * P16_BOX_BYTES, &mapA, p.core.a_mn, a_row + 64 * b, t.a_z, pl);
+                                copy(sa + pl * R::A_PLANE + b * P16_BOX_BYTES, mapA, a_mn, a_row + 64 * b, t.a_z, pl);
 #pragma unroll
                             for (int b = 0; b < R::B_BOXES; ++b)
-                                if (b < b_boxes) copy(sb + pl * R::B_PLANE + b * R::B_BOX_BYTES, &mapB, p.core.b_mn, b_row + 64 * b, t.b_z, pl);
+                                if (b < b_boxes) copy(sb + pl * R::B_PLANE + b * R::B_BOX_BYTES, mapB, b_mn, b_row + 64 * b, t.b_z, pl);
                         }
                     }
                     if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                 }
             }
+            }
         } else if (warp == 1 && rank == 0) {
             // -------------------------------------------------------- MMAs
-            const uint32_t step_a = p.core.a_mn ? 2048 >> 4 : 32 >> 4, step_b = p.core.b_mn ? 2048 >> 4 : 32 >> 4;   // 16 inner indices on
             int slot = 0;
             uint32_t slot_phase = 0;
+            for (int ph = 0, phases = P::phases(p); ok && ph < phases; ++ph) {
+            const int64_t total = P::template total<CG, BN>(p, table, ph);
             for (int64_t item = first_item; ok && item < total; item += item_step) {
-                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, ph, item);
                 const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
-                const uint32_t idesc = p.core.idesc | (static_cast<uint32_t>(t.cols >> 3) << 17);
                 for (int kb0 = first_block(blocks), end = end_block(blocks); ok && kb0 < end; kb0 += p.core.seg) {
                     ok = wait(tempty_bar + 8 * slot, ((slot_phase >> slot) & 1u) ^ 1u);
                     if (!ok) break;
@@ -282,7 +290,11 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t sa = ring + stage * R::STAGE, sb = sa + PLANES * R::A_PLANE;
-                        const uint64_t a = smem_desc16(sa, p.core.a_mn), b = smem_desc16(sb, p.core.b_mn);
+                        const int a_mn = P::a_mn(p, t, kb), b_mn = P::b_mn(p, t, kb);
+                        const uint64_t a = smem_desc16(sa, a_mn), b = smem_desc16(sb, b_mn);
+                        const uint32_t step_a = a_mn ? 2048 >> 4 : 32 >> 4, step_b = b_mn ? 2048 >> 4 : 32 >> 4;      // 16 inner indices on
+                        const uint32_t idesc = p.core.idesc | (static_cast<uint32_t>(a_mn) << 15) | (static_cast<uint32_t>(b_mn) << 16) |
+                                               (static_cast<uint32_t>(t.cols >> 3) << 17);
                         const int left = t.k_len - kb * P16_BLOCK_K;
                         if (leader) {
                             if constexpr (PLANES == 2) {
@@ -315,11 +327,13 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
                     slot ^= 1;
                 }
             }
+            }
         } else if (P::RAGGED_K && warp == 2) {
             // -------------------------------------------------------- inner indices behind the group's end
             uint32_t tail_phase = 0;                         // bit s: phase of stage s's tail barrier
+            const int64_t total = P::template total<CG, BN>(p, table, 0);
             for (int64_t item = first_item; ok && item < total; item += item_step) {
-                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
+                const typename P::Tile t = P::template decode<CG, BN>(p, table, 0, item);
                 const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
                 const int mine = end_block(blocks) - first_block(blocks);
                 const int last = (stage + mine - 1) % STAGES;
@@ -388,19 +402,27 @@ product16_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant
         return true;
     };
     if constexpr (SPLIT == 1) {
-        if (warp >= P16_FIRST_EPI)
-            for (int64_t item = first_item; item < total; item += item_step) {
-                const typename P::Tile t = P::template decode<CG, BN>(p, table, item);
-                if (!collect(t)) break;
-                P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS);
+        if (warp >= P16_FIRST_EPI) {
+            // (a warp that has given up goes through the phases all the same: done() is where the warps of a block meet)
+            bool ok = true;
+            for (int ph = 0, phases = P::phases(p); ph < phases; ++ph) {
+                ok = ok && P::ready(p, ph, abort_flag);
+                const int64_t total = P::template total<CG, BN>(p, table, ph);
+                for (int64_t item = first_item; ok && item < total; item += item_step) {
+                    const typename P::Tile t = P::template decode<CG, BN>(p, table, ph, item);
+                    ok = collect(t);
+                    if (ok) P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS);
+                }
+                P::done(p, ph);
             }
+        }
     } else {
         constexpr int OWN = R::COLS / SPLIT;
-        const bool works = warp >= P16_FIRST_EPI && first_item < total;
+        const bool works = warp >= P16_FIRST_EPI && first_item < P::template total<CG, BN>(p, table, 0);
         typename P::Tile t;
         bool ok = works;
         if (works) {
-            t = P::template decode<CG, BN>(p, table, first_item);
+            t = P::template decode<CG, BN>(p, table, 0, first_item);
             ok = collect(t);
         }
         // box of a warp and a sender: [column][lane]
@@ -474,8 +496,7 @@ inline bool make_pair_map16(CUtensorMap *map, const void *base, int64_t chunks, 
 }
 
 template <class P, int CG, int BN, int PLANES, int SPLIT>
-oz_status_t launch_product16(const CUtensorMap &mapA, const CUtensorMap &mapB, const typename P::Params &p, int64_t most_tiles,
-                             size_t table_bytes, cudaStream_t stream)
+oz_status_t launch_product16(const typename P::Maps &maps, const typename P::Params &p, int64_t most_tiles, size_t table_bytes, cudaStream_t stream)
 {
     auto kernel = product16_kernel<P, CG, BN, PLANES, SPLIT>;
     static std::atomic<unsigned long long> ready{0};
@@ -494,11 +515,17 @@ oz_status_t launch_product16(const CUtensorMap &mapA, const CUtensorMap &mapB, c
     attr[0].val.clusterDim.x = CG * SPLIT;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    if (P::COOPERATIVE) {
+        // blocks that wait for one another are on the device together
+        attr[1].id = cudaLaunchAttributeCooperative;
+        attr[1].val.cooperative = 1;
+    } else {
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+    }
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    OZ_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, mapA, mapB, p));
+    OZ_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, maps, p));
     count_launch();
     return OZ_OK;
 }
