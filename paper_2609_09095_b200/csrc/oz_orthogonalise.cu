@@ -31,17 +31,14 @@ namespace {
 
 constexpr int kMaxSteps = 100;
 constexpr int NORM_THREADS = 256;
-constexpr int MAX_PARTS = 64;                      // partial sums of squares of a matrix
+constexpr int MAX_PARTS = 296;                     // partial sums of squares of a matrix
 constexpr int PLANE_TILE = 64;
 constexpr unsigned long long kPhaseLimitNs = 4000000000ull;        // wait for the other blocks
 
-__device__ __forceinline__ float load_number(const void *X, int64_t at, int type)
-{
-    if (type == OZ_F32) return static_cast<const float *>(X)[at];
-    if (type == OZ_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(X)[at]);
-    return __half2float(static_cast<const __half *>(X)[at]);
-}
-
+template <class T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_float(float v) { return v; }
 template <class T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
@@ -80,20 +77,55 @@ struct MatrixParams {
 // where element i of a line of plane pairs lies; its lo half is 64 numbers on
 __device__ __forceinline__ int pair_at(int i) { return (i >> 6) * 128 + (i & 63); }
 
-// Sums of squares, in double: any finite FP32 number squares without overflow, and the order is fixed.
-__global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const MatrixParams p)
+// Sums of squares, in double: any finite FP32 number squares without overflow, and the order is fixed.  Columns of `column` elements are read
+// 16 bytes at a time where their addresses allow.
+template <class T>
+__global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const MatrixParams p, int64_t column, int64_t columns, int wide)
 {
     __shared__ double warp_sums[NORM_THREADS / 32];
     dependency_release();
     dependency_wait();
     const int64_t matrix = blockIdx.x / p.parts;
     const int part = blockIdx.x % p.parts;
-    const int64_t total = p.m * p.n;
+    constexpr int V = 16 / sizeof(T), UNROLL = 4;
+    const T *G = static_cast<const T *>(p.G) + matrix * p.strideG;
     double sum = 0.0;
-    for (int64_t e = part * NORM_THREADS + threadIdx.x; e < total; e += p.parts * NORM_THREADS) {
-        const int64_t j = total <= 0xFFFFFFFFll ? static_cast<uint32_t>(e) / static_cast<uint32_t>(p.m) : e / p.m;
-        const double v = load_number(p.G, matrix * p.strideG + (e - j * p.m) + j * p.ldg, p.type);
-        sum = fma(v, v, sum);
+    const int64_t step = static_cast<int64_t>(p.parts) * NORM_THREADS;
+    if (wide) {
+        const int64_t each = (column + V - 1) / V, total = each * columns;       // pieces of V elements
+        for (int64_t e0 = part * NORM_THREADS + threadIdx.x; e0 < total; e0 += UNROLL * step) {
+            __align__(16) T v[UNROLL][V];
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                const int64_t e = e0 + u * step;
+                *reinterpret_cast<uint4 *>(v[u]) = make_uint4(0u, 0u, 0u, 0u);
+                if (e < total) {
+                    const int64_t j = total <= 0xFFFFFFFFll ? static_cast<uint32_t>(e) / static_cast<uint32_t>(each) : e / each, i = (e - j * each) * V;
+                    const T *from = G + i + j * p.ldg;
+                    if (i + V <= column) {
+                        *reinterpret_cast<uint4 *>(v[u]) = *reinterpret_cast<const uint4 *>(from);
+                    } else {
+                        for (int k = 0; k < V; ++k)
+                            if (i + k < column) v[u][k] = from[k];
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const double x = to_float(v[u][k]);
+                    sum = fma(x, x, sum);
+                }
+        }
+    } else {
+        const int64_t total = column * columns;
+#pragma unroll 4
+        for (int64_t e = part * NORM_THREADS + threadIdx.x; e < total; e += step) {
+            const int64_t j = total <= 0xFFFFFFFFll ? static_cast<uint32_t>(e) / static_cast<uint32_t>(column) : e / column;
+            const double x = to_float(G[(e - j * column) + j * p.ldg]);
+            sum = fma(x, x, sum);
+        }
     }
     for (int d = 16; d > 0; d /= 2) sum += __shfl_down_sync(0xFFFFFFFFu, sum, d);
     if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = sum;
@@ -105,62 +137,126 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const MatrixParams p
     }
 }
 
-// 1 / (|G|_F + eps); 0 for a matrix of zeros; NaN, which the whole update then is, for one that holds Inf or NaN.  One warp.
-__device__ double inverse_norm(const MatrixParams &p, int64_t matrix)
+// 1 / (|G|_F + eps) times `scale`, as two factors; 0 for a matrix of zeros; NaN, which the whole update then is, for one that holds Inf or
+// NaN.  The first is a power of two, so that a product with both is rounded once, and neither the number nor what it passes through leaves the
+// range of FP32, from the smallest numbers to the largest.  One warp.
+__device__ float2 inverse_norm(const MatrixParams &p, int64_t matrix, double scale)
 {
     double sum = 0.0;
     for (int i = threadIdx.x % 32; i < p.parts; i += 32) sum += p.sums[matrix * p.parts + i];
     for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
     if (!(sum <= 1.7e308)) {
         atomicOr(p.status, 1u << OZ_ERR_NONFINITE_INPUT);
-        return nan("");
+        return make_float2(nanf(""), 1.0f);
     }
-    return sum > 0.0 ? 1.0 / (sqrt(sum) + p.eps) : 0.0;
+    if (sum == 0.0) return make_float2(0.0f, 0.0f);
+    const double f = scale / (sqrt(sum) + p.eps);
+    const int half = ilogb(f) / 2;
+    return make_float2(ldexpf(1.0f, half), static_cast<float>(ldexp(f, -half)));
 }
 
-// Planes of X, tiles of 64 x 64 through shared memory where X is the transpose of G.  PLANES = false: no step follows, X itself
-// goes to O, in G's own direction.
-template <bool PLANES>
-__global__ void __launch_bounds__(256) planes_kernel(const MatrixParams p)
+// Planes of X, tiles of 64 x 64; a lane has two consecutive rows, a warp eight columns.  Through shared memory where X is the transpose of
+// G.  PLANES = false: no step follows, X itself goes to O, in G's own direction.
+template <class T, bool PLANES>
+__global__ void __launch_bounds__(256) planes_kernel(const MatrixParams p, int tiles, int pairs)
 {
     __shared__ float tile[PLANE_TILE][PLANE_TILE + 1];
-    __shared__ double factor;
+    __shared__ float2 factor;
     dependency_release();
     dependency_wait();
-    const int64_t rows = p.m, cols = p.n;
-    const int64_t tiles_m = (rows + PLANE_TILE - 1) / PLANE_TILE, each = tiles_m * ((cols + PLANE_TILE - 1) / PLANE_TILE);
-    const int64_t matrix = blockIdx.x / each, t = blockIdx.x % each;
-    const int64_t i0 = t % tiles_m * PLANE_TILE, j0 = t / tiles_m * PLANE_TILE;
-    if (threadIdx.x < 32) {
-        const double f = inverse_norm(p, matrix);
-        if (threadIdx.x == 0) factor = f;
-    }
-    __syncthreads();
-    const double f = PLANES ? factor * static_cast<double>(p.scale) : factor;
-    const int ti = threadIdx.x % PLANE_TILE, tj = threadIdx.x / PLANE_TILE;
+    const uint32_t tiles_m = static_cast<uint32_t>((p.m + PLANE_TILE - 1) / PLANE_TILE);
+    const uint32_t each = tiles_m * static_cast<uint32_t>((p.n + PLANE_TILE - 1) / PLANE_TILE);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    struct __align__(2 * sizeof(T)) Pair {
+        T a, b;
+    };
+    int64_t known = -1;
+    for (uint32_t item = blockIdx.x; item < static_cast<uint32_t>(tiles); item += gridDim.x) {
+        const uint32_t matrix = item / each, t = item - matrix * each, tj = t / tiles_m;
+        const int64_t i0 = static_cast<int64_t>(t - tj * tiles_m) * PLANE_TILE, j0 = static_cast<int64_t>(tj) * PLANE_TILE;
+        const T *G = static_cast<const T *>(p.G) + matrix * p.strideG + i0 + 2 * lane + (j0 + warp) * p.ldg;
+        const int rows = static_cast<int>(min(p.m - i0, static_cast<int64_t>(PLANE_TILE))) - 2 * lane;      // from the lane's first on
+        const int cols = static_cast<int>(min(p.n - j0, static_cast<int64_t>(PLANE_TILE))) - warp;
+        float v[8][2];
 #pragma unroll
-    for (int s = 0; s < PLANE_TILE; s += 4) {
-        const int64_t i = i0 + ti, j = j0 + tj + s;
-        float v = 0.0f;
-        if (i < rows && j < cols) {
-            v = static_cast<float>(static_cast<double>(load_number(p.G, matrix * p.strideG + i + j * p.ldg, p.type)) * f);
-            if (!PLANES) store_number(p.O, matrix * p.strideO + i + j * p.ldo, v, p.otype);
+        for (int s = 0; s < 8; ++s) {
+            const T *from = G + 8 * s * p.ldg;
+            v[s][0] = v[s][1] = 0.0f;
+            if (8 * s < cols) {
+                if (pairs && rows > 1) {
+                    const Pair two = *reinterpret_cast<const Pair *>(from);
+                    v[s][0] = to_float(two.a);
+                    v[s][1] = to_float(two.b);
+                } else {
+                    if (rows > 0) v[s][0] = to_float(from[0]);
+                    if (rows > 1) v[s][1] = to_float(from[1]);
+                }
+            }
         }
-        if (PLANES) tile[tj + s][ti] = v;
-    }
-    if (!PLANES) return;
-    __syncthreads();
-    const int64_t x0 = p.transposed ? j0 : i0, y0 = p.transposed ? i0 : j0;       // first row and column of X
+        __syncthreads();                                     // the tile and the factor of the round before are no longer read
+        if (matrix != known) {
+            if (threadIdx.x < 32) {
+                const float2 f = inverse_norm(p, matrix, PLANES ? static_cast<double>(p.scale) : 1.0);
+                if (threadIdx.x == 0) factor = f;
+            }
+            __syncthreads();
+            known = matrix;
+        }
+        const float2 f = factor;
 #pragma unroll
-    for (int s = 0; s < PLANE_TILE; s += 4) {
-        // rows behind the last are written too: the tile holds zeros there
-        const int64_t x = x0 + ti, y = y0 + tj + s;
-        const float v = p.transposed ? tile[ti][tj + s] : tile[tj + s][ti];
-        if (y < p.c) {
-            __half *to = p.X + (matrix * p.c + y) * p.ld + pair_at(static_cast<int>(x));
-            split_planes(v, to, to + 64);
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) v[s][k] = k < rows && 8 * s < cols ? v[s][k] * f.x * f.y : 0.0f;
+        if constexpr (!PLANES) {
+            const int64_t at = matrix * p.strideO + i0 + 2 * lane + (j0 + warp) * p.ldo;
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (k < rows && 8 * s < cols) store_number(p.O, at + k + 8 * s * p.ldo, v[s][k], p.otype);
+        } else {
+            if (p.transposed) {
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) tile[warp + 8 * s][2 * lane + k] = v[s][k];
+                __syncthreads();
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) v[s][k] = tile[2 * lane + k][warp + 8 * s];
+            }
+            // (rows behind the last are written too: zeros)
+            const int64_t x0 = p.transposed ? j0 : i0, y0 = (p.transposed ? i0 : j0) + warp;               // first row, the warp's first column of X
+            __half *to = p.X + (matrix * static_cast<int64_t>(p.c) + y0) * p.ld + pair_at(static_cast<int>(x0)) + 2 * lane;
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (y0 + 8 * s < p.c) {
+                    __half2 hi, lo;
+                    split_planes(v[s][0], &hi.x, &lo.x);
+                    split_planes(v[s][1], &hi.y, &lo.y);
+                    *reinterpret_cast<__half2 *>(to + 8 * s * static_cast<int64_t>(p.ld)) = hi;
+                    *reinterpret_cast<__half2 *>(to + 8 * s * static_cast<int64_t>(p.ld) + 64) = lo;
+                }
         }
     }
+}
+
+template <class T>
+oz_status_t launch_planes(const MatrixParams &p, bool planes, cudaStream_t stream)
+{
+    const bool flat = p.ldg == p.m;
+    const int64_t column = flat ? p.m * p.n : p.m, columns = flat ? 1 : p.n;
+    const int wide = reinterpret_cast<uintptr_t>(p.G) % 16 == 0 && (columns == 1 || p.ldg * sizeof(T) % 16 == 0) &&
+                     (p.count == 1 || p.strideG * sizeof(T) % 16 == 0);
+    const int pairs = reinterpret_cast<uintptr_t>(p.G) % (2 * sizeof(T)) == 0 && p.ldg % 2 == 0 && (p.count == 1 || p.strideG % 2 == 0);
+    const int64_t tiles = p.count * ((p.m + PLANE_TILE - 1) / PLANE_TILE) * ((p.n + PLANE_TILE - 1) / PLANE_TILE), most = 8 * sm_count();
+    if (tiles > 0x7FFFFFFF - most) return OZ_ERR_UNSUPPORTED;
+    OZ_CUDA_CHECK(launch(norm_kernel<T>, dim3(static_cast<unsigned>(p.count * p.parts)), NORM_THREADS, 0, stream, p, column, columns, wide));
+    OZ_CUDA_CHECK(launch(planes ? planes_kernel<T, true> : planes_kernel<T, false>, dim3(static_cast<unsigned>(tiles < most ? tiles : most)), 256, 0,
+                         stream, p, static_cast<int>(tiles), pairs));
+    count_launch(2);
+    return OZ_OK;
 }
 
 // ---------------------------------------------------------------- products
@@ -174,8 +270,23 @@ struct NewtonParams {
     int otype, transposed;
     unsigned int *arrived;          // blocks that have finished a phase, all phases together
     Core16 core;
-    float alpha[3 * kMaxSteps], beta[3 * kMaxSteps];      // of each phase: result = alpha accumulator + beta old
+    float alpha[3 * kMaxSteps], beta[3 * kMaxSteps];      // of each phase: result = alpha accumulator + beta S or beta X
+    float diagonal[kMaxSteps];      // of P: + diagonal I, where a X is taken in through P
 };
+
+struct NewtonMaps {
+    CUtensorMap x[2], gram, poly;
+};
+
+// tiles of a matrix in a phase: all of X, or those of S and P that touch the lower blocks of 256
+template <int BN>
+__host__ __device__ __forceinline__ uint32_t newton_tiles(int r, int c, int phase)
+{
+    const uint32_t tm = static_cast<uint32_t>((r + 255) / 256), wide = 256 / BN;
+    if (phase % 3 == kApply) return tm * static_cast<uint32_t>((c + BN - 1) / BN);
+    const uint32_t last = (static_cast<uint32_t>(r) - 256 * (tm - 1) + BN - 1) / BN;              // columns of tiles of the last block
+    return wide * tm * (tm - 1) / 2 + (tm - 1) * wide + last;
+}
 
 // All steps in one launch: phase 3 s is S = X X^T of step s, 3 s + 1 P, 3 s + 2 the new X.  The blocks meet between the phases.
 // Tiles are 256 rows x BN columns by pairs: the three plane products of a block read shared memory at 106 bytes a cycle with BN = 256; those of
@@ -183,11 +294,11 @@ struct NewtonParams {
 // Of S and P only blocks of 256 x 256 on and below the diagonal are computed and stored, line j holding elements i >= j (and all of the
 // diagonal block).  A product that wants a block above takes the one below with its directions exchanged: an operand stored along its rows
 // instead of along the inner dimension, which the tensor core reads as well.
+// FOLDED: a X is taken in through P's diagonal, and results are 16-bit numbers (see oz_orthogonalise()).
+template <bool FOLDED>
 struct NewtonPolicy {
     using Params = NewtonParams;
-    struct Maps {
-        CUtensorMap x[2], gram, poly;
-    };
+    using Maps = NewtonMaps;
     struct Tile : Tile16 {
         int matrix, phase;
     };
@@ -204,57 +315,58 @@ struct NewtonPolicy {
     static __device__ __forceinline__ void setup(const Params &, int, int *) {}
     static __device__ __forceinline__ int phases(const Params &p) { return 3 * p.steps; }
 
-    // Blocks arrive with a release after all their stores, and whoever goes on acquires; the fences carry the stores over to the bulk copies.
+    // A block arrives with a release, cumulative over what its threads have stored before they met, and whoever goes on acquires; the proxy fences
+    // carry the stores over to the bulk copies.  (Every thread with a fence of its own: 1.2 to 1.9 us.)
     static __device__ __forceinline__ bool ready(const Params &p, int phase, volatile int *abort_flag)
     {
-        if (phase == 0) return true;
         const unsigned int want = static_cast<unsigned int>(phase) * gridDim.x;
         unsigned long long start = 0;
-        for (unsigned int poll = 0;; ++poll) {
-            unsigned int have;
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(p.arrived) : "memory");
-            if (__all_sync(0xFFFFFFFFu, have >= want)) break;
-            if (*abort_flag) return false;
-            if (poll % 256 == 255) {
-                const unsigned long long now = global_timer_ns();
-                if (start == 0) start = now;
-                if (__any_sync(0xFFFFFFFFu, now - start > kPhaseLimitNs)) {
-                    *abort_flag = 1;
-                    atomicOr(p.core.status, 1u << OZ_ERR_TIMEOUT);
-                    return false;
+        bool ok = true;
+        if (threadIdx.x % 32 == 0) {
+            for (unsigned int poll = 0;; ++poll) {
+                unsigned int have;
+                asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(p.arrived) : "memory");
+                if (have >= want) break;
+                if (*abort_flag) {
+                    ok = false;
+                    break;
+                }
+                if (poll % 256 == 255) {
+                    const unsigned long long now = global_timer_ns();
+                    if (start == 0) start = now;
+                    if (now - start > kPhaseLimitNs) {
+                        *abort_flag = 1;
+                        atomicOr(p.core.status, 1u << OZ_ERR_TIMEOUT);
+                        ok = false;
+                        break;
+                    }
                 }
             }
         }
+        ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
         asm volatile("fence.proxy.async;" ::: "memory");
-        return true;
+        return ok;
     }
     static __device__ __forceinline__ void done(const Params &p, int)
     {
-        __threadfence();
         asm volatile("fence.proxy.async;" ::: "memory");
         asm volatile("bar.sync 1, %0;" ::"n"(P16_EPI_WARPS * 32) : "memory");
-        if (threadIdx.x == 32 * P16_FIRST_EPI) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.arrived) : "memory");
+        if (threadIdx.x == 32 * P16_FIRST_EPI) {
+            __threadfence();
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.arrived) : "memory");
+        }
     }
 
-    // tiles of a matrix: all of X, or those of S and P that touch the lower blocks of 256
-    template <int BN>
-    static __host__ __device__ __forceinline__ uint32_t tiles_each(int r, int c, int phase)
-    {
-        const uint32_t tm = static_cast<uint32_t>((r + 255) / 256), wide = 256 / BN;
-        if (phase % 3 == kApply) return tm * static_cast<uint32_t>((c + BN - 1) / BN);
-        const uint32_t last = (static_cast<uint32_t>(r) - 256 * (tm - 1) + BN - 1) / BN;          // columns of tiles of the last block
-        return wide * tm * (tm - 1) / 2 + (tm - 1) * wide + last;
-    }
     template <int CG, int BN>
     static __device__ __forceinline__ int64_t total(const Params &p, const int *, int phase)
     {
-        return static_cast<int64_t>(p.count) * tiles_each<BN>(p.r, p.c, phase);
+        return static_cast<int64_t>(p.count) * newton_tiles<BN>(p.r, p.c, phase);
     }
 
     template <int CG, int BN>
     static __device__ __forceinline__ Tile decode(const Params &p, const int *, int phase, int64_t item)
     {
-        const uint32_t each = tiles_each<BN>(p.r, p.c, phase);
+        const uint32_t each = newton_tiles<BN>(p.r, p.c, phase);
         Tile t;
         t.phase = phase;
         t.matrix = static_cast<int>(static_cast<uint32_t>(item) / each);
@@ -296,45 +408,46 @@ struct NewtonPolicy {
     template <int CG, int BN, int N>
     static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col)
     {
-        const int i = t.a_row + row, j0 = t.b_row + col, lines = t.phase % 3 == kApply ? p.c : p.r, left = lines - j0;
+        const int left = (t.phase % 3 == kApply ? p.c : p.r) - t.b_row - col;
+        if (left >= N) store_columns<true>(p, t, acc, t.a_row + row, t.b_row + col, left);
+        else if (left > 0) store_columns<false>(p, t, acc, t.a_row + row, t.b_row + col, left);
+    }
+
+    template <bool FULL, int N>
+    static __device__ __forceinline__ void store_columns(const Params &p, const Tile &t, const float (&acc)[N], int i, int j0, int left)
+    {
         const bool last = t.phase == 3 * p.steps - 1;
-        if (i >= (last ? p.r : p.ld / 2) || left <= 0) return;
+        if (i >= (last ? p.r : p.ld / 2)) return;
         const float alpha = p.alpha[t.phase], beta = p.beta[t.phase];
-        const int64_t at = (static_cast<int64_t>(t.matrix) * lines + j0) * p.ld + pair_at(i);
-        const int from = t.phase / 3 & 1;
+        const int64_t at = (static_cast<int64_t>(t.matrix) * (t.phase % 3 == kApply ? p.c : p.r) + j0) * p.ld + pair_at(i);
+        const __half *x = p.x[t.phase / 3 & 1] + at;
         if (last) {
-            const __half *old = p.x[from] + at;
             auto as = [&](auto *O) {
                 O += t.matrix * p.strideO;
-                if (p.transposed) {
-                    if (left >= N) store_last<true, true>(p, old, O + j0 + i * p.ldo, acc, alpha, beta, left);
-                    else store_last<false, true>(p, old, O + j0 + i * p.ldo, acc, alpha, beta, left);
-                } else {
-                    if (left >= N) store_last<true, false>(p, old, O + i + j0 * p.ldo, acc, alpha, beta, left);
-                    else store_last<false, false>(p, old, O + i + j0 * p.ldo, acc, alpha, beta, left);
-                }
+                if (p.transposed) store_last<FULL, true, !FOLDED>(p, x, O + j0 + i * p.ldo, acc, alpha, beta, left);
+                else store_last<FULL, false, !FOLDED>(p, x, O + i + j0 * p.ldo, acc, alpha, beta, left);
             };
-            if (p.otype == OZ_F32) as(static_cast<float *>(p.O));
+            if constexpr (!FOLDED) as(static_cast<float *>(p.O));
             else if (p.otype == OZ_BF16) as(static_cast<__nv_bfloat16 *>(p.O));
             else as(static_cast<__half *>(p.O));
         } else if (t.phase % 3 == kGram) {
-            if (left >= N) store_planes<true, false>(p, nullptr, p.gram + at, acc, alpha, beta, left);
-            else store_planes<false, false>(p, nullptr, p.gram + at, acc, alpha, beta, left);
+            store_planes<FULL, false>(p, nullptr, p.gram + at, acc, alpha, beta, 0.0f, 0, left);
+        } else if (t.phase % 3 == kPolynomial) {
+            store_planes<FULL, true>(p, p.gram + at, p.poly + at, acc, alpha, beta, i < p.r ? p.diagonal[t.phase / 3] : 0.0f, i - j0, left);
         } else {
-            const __half *old = (t.phase % 3 == kPolynomial ? p.gram : p.x[from]) + at;
-            __half *to = (t.phase % 3 == kPolynomial ? p.poly : p.x[from ^ 1]) + at;
-            if (left >= N) store_planes<true, true>(p, old, to, acc, alpha, beta, left);
-            else store_planes<false, true>(p, old, to, acc, alpha, beta, left);
+            store_planes<FULL, !FOLDED>(p, x, p.x[(t.phase / 3 & 1) ^ 1] + at, acc, alpha, beta, 0.0f, -1, left);
         }
     }
 
-    // v = alpha acc + beta old of columns c0 .. c0 + 7; `old` moves on.  (Written by other blocks in this launch: from L2.)
+    // v = alpha acc + beta old of columns c0 .. c0 + 7; `old` moves on.  (Written by other blocks of this launch: from L2.)
     template <bool FULL, bool OLD, int N>
     static __device__ __forceinline__ void results(float (&v)[8], const __half *&old, int64_t ld, const float (&acc)[N], int c0, float alpha,
                                                    float beta, int left)
     {
-        __half hi[8], lo[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = alpha * acc[c0 + c];
         if constexpr (OLD) {
+            __half hi[8], lo[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 const bool inside = FULL || c0 + c < left;
@@ -342,16 +455,15 @@ struct NewtonPolicy {
                 lo[c] = inside ? __ldcg(old + 64) : __half();
                 old += ld;
             }
-        }
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            v[c] = alpha * acc[c0 + c];
-            if constexpr (OLD) v[c] = fmaf(beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
+            for (int c = 0; c < 8; ++c) v[c] = fmaf(beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
         }
     }
 
+    // planes of the results, at column `on` of the thread's + diagonal
     template <bool FULL, bool OLD, int N>
-    static __device__ __forceinline__ void store_planes(const Params &p, const __half *old, __half *to, const float (&acc)[N], float alpha, float beta, int left)
+    static __device__ __forceinline__ void store_planes(const Params &p, const __half *old, __half *to, const float (&acc)[N], float alpha, float beta,
+                                                        float diagonal, int on, int left)
     {
         static_assert(N % 8 == 0, "columns eight at a time");
 #pragma unroll
@@ -360,46 +472,53 @@ struct NewtonPolicy {
             results<FULL, OLD>(v, old, p.ld, acc, c0, alpha, beta, left);
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
+                if (FOLDED && OLD && c0 + c == on) v[c] += diagonal;
                 if (FULL || c0 + c < left) split_planes(v[c], to, to + 64);
                 to += p.ld;
             }
         }
     }
 
-    // the result itself: down its columns, or, transposed, the row's consecutive elements
-    template <bool FULL, bool TRANSPOSED, int N, class T>
+    // the results themselves: down their columns, or, transposed, the row's consecutive elements
+    template <bool FULL, bool TRANSPOSED, bool OLD, int N, class T>
     static __device__ __forceinline__ void store_last(const Params &p, const __half *old, T *to, const float (&acc)[N], float alpha, float beta, int left)
     {
         const bool wide = TRANSPOSED && FULL && reinterpret_cast<uintptr_t>(to) % 16 == 0;
 #pragma unroll
         for (int c0 = 0; c0 < N; c0 += 8) {
             float v[8];
-            results<FULL, true>(v, old, p.ld, acc, c0, alpha, beta, left);
+            results<FULL, OLD>(v, old, p.ld, acc, c0, alpha, beta, left);
             __align__(16) T w[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) w[c] = from_float<T>(v[c]);
             if (wide) {
 #pragma unroll
                 for (int c = 0; c < static_cast<int>(sizeof(T)) / 2; ++c) reinterpret_cast<uint4 *>(to + c0)[c] = reinterpret_cast<const uint4 *>(w)[c];
-            } else {
+            } else if (TRANSPOSED) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
-                    if (FULL || c0 + c < left) to[TRANSPOSED ? c0 + c : (c0 + c) * p.ldo] = w[c];
+                    if (FULL || c0 + c < left) to[c0 + c] = w[c];
+            } else {
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    if (FULL || c0 + c < left) *to = w[c];
+                    to += p.ldo;
+                }
             }
         }
     }
 };
 
-template <int BN>
-oz_status_t launch_newton(const NewtonPolicy::Maps &maps, const NewtonParams &p, cudaStream_t stream)
+template <bool FOLDED, int BN>
+oz_status_t launch_newton(const NewtonMaps &maps, const NewtonParams &p, cudaStream_t stream)
 {
     int64_t most = 0;
     for (int phase = 0; phase < 3; ++phase) {
-        const int64_t tiles = static_cast<int64_t>(p.count) * NewtonPolicy::tiles_each<BN>(p.r, p.c, phase);
+        const int64_t tiles = static_cast<int64_t>(p.count) * newton_tiles<BN>(p.r, p.c, phase);
         if (tiles > most) most = tiles;
     }
     if (most >= (1ll << 31)) return OZ_ERR_UNSUPPORTED;
-    return launch_product16<NewtonPolicy, 2, BN, 2, 1>(maps, p, most, 0, stream);
+    return launch_product16<NewtonPolicy<FOLDED>, 2, BN, 2, 1>(maps, p, most, 0, stream);
 }
 
 // cycles of a step with tiles of 256 x BN: rounds over the pairs, blocks of 64 inner indices at `each` cycles
@@ -408,7 +527,7 @@ int64_t step_cycles(const NewtonParams &p, int each)
 {
     int64_t sum = 0;
     for (int phase = 0; phase < 3; ++phase) {
-        const int64_t tiles = static_cast<int64_t>(p.count) * NewtonPolicy::tiles_each<BN>(p.r, p.c, phase), pairs = sm_count() / 2;
+        const int64_t tiles = static_cast<int64_t>(p.count) * newton_tiles<BN>(p.r, p.c, phase), pairs = sm_count() / 2;
         sum += (tiles + pairs - 1) / pairs * (((phase == kGram ? p.c : p.r) + 63) / 64 * each);
     }
     return sum;
@@ -427,8 +546,9 @@ Layout layout_of(int64_t m, int64_t n, int64_t count)
     l.r = m < n ? m : n;
     l.c = m < n ? n : m;
     l.chunks = (l.r + 63) / 64;
-    const int64_t pieces = (m * n + NORM_THREADS * 16 - 1) / (NORM_THREADS * 16);
-    l.parts = static_cast<int>(pieces < MAX_PARTS ? pieces : MAX_PARTS);
+    // pieces of 16 elements a thread, two blocks a multiprocessor in all
+    const int64_t pieces = (m * n + NORM_THREADS * 16 - 1) / (NORM_THREADS * 16), share = (MAX_PARTS + count - 1) / count;
+    l.parts = static_cast<int>(pieces < share ? pieces : share);
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t here = at;
@@ -470,12 +590,13 @@ double largest_value(double a, double b, double c, double bound)
     return most;
 }
 
-// the largest |b q + c q^2| of 0 <= q <= bound
-double largest_polynomial(double b, double c, double bound)
+// the largest |a + b q + c q^2| of 0 <= q <= bound
+double largest_polynomial(double a, double b, double c, double bound)
 {
-    double most = std::fabs(bound * (b + bound * c));
+    auto value = [&](double q) { return std::fabs(a + q * (b + q * c)); };
+    double most = value(0.0) > value(bound) ? value(0.0) : value(bound);
     const double q = c != 0.0 ? -b / (2.0 * c) : -1.0;
-    if (q > 0.0 && q < bound && std::fabs(q * (b + q * c)) > most) most = std::fabs(q * (b + q * c));
+    if (q > 0.0 && q < bound && value(q) > most) most = value(q);
     return most;
 }
 
@@ -514,9 +635,10 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     double bound[kMaxSteps + 1] = {1.0};
     const double a = steps ? coefficients[0] : 0.0, b = steps ? coefficients[1] : 0.0, c = steps ? coefficients[2] : 0.0;
     if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return OZ_ERR_INVALID_ARG;
+    const bool folded = otype != OZ_F32;
     for (int s = 0; s < steps; ++s) {
         bound[s + 1] = largest_value(a, b, c, bound[s]);
-        const double poly = largest_polynomial(b, c, bound[s] * bound[s]);
+        const double poly = largest_polynomial(folded ? a : 0.0, b, c, bound[s] * bound[s]);
         if (!(bound[s + 1] <= 0x1p30) || !(poly <= 0x1p60) || (bound[s + 1] < 0x1p-30)) return OZ_ERR_UNSUPPORTED;
     }
     if (m == 0 || n == 0 || count == 0) return OZ_OK;
@@ -532,7 +654,7 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     char *ws = static_cast<char *>(workspace);
     __half *x[2] = {reinterpret_cast<__half *>(ws + l.x[0]), reinterpret_cast<__half *>(ws + l.x[1])};
     __half *gram = reinterpret_cast<__half *>(ws + l.s), *poly = reinterpret_cast<__half *>(ws + l.poly);
-    NewtonPolicy::Maps maps;
+    NewtonMaps maps;
     if (steps && !(make_pair_map16(&maps.x[0], x[0], l.chunks, l.c, count) && make_pair_map16(&maps.x[1], x[1], l.chunks, l.c, count) &&
                    make_pair_map16(&maps.gram, gram, l.chunks, l.r, count) && make_pair_map16(&maps.poly, poly, l.chunks, l.r, count)))
         return OZ_ERR_CUDA;
@@ -560,12 +682,10 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     mp.scale = static_cast<float>(plane_scale(bound[0]));
     mp.X = x[0];
     mp.status = device_status_word();
-    const int64_t tiles = count * ((m + PLANE_TILE - 1) / PLANE_TILE) * ((n + PLANE_TILE - 1) / PLANE_TILE);
-    if (tiles > 0x7FFFFFFF || count * l.parts > 0x7FFFFFFF) return OZ_ERR_UNSUPPORTED;
-    OZ_CUDA_CHECK(launch(norm_kernel, dim3(static_cast<unsigned>(count * l.parts)), NORM_THREADS, 0, s, mp));
-    OZ_CUDA_CHECK(launch(steps ? planes_kernel<true> : planes_kernel<false>, dim3(static_cast<unsigned>(tiles)), 256, 0, s, mp));
-    count_launch(2);
-
+    if (count * l.parts > 0x7FFFFFFF) return OZ_ERR_UNSUPPORTED;
+    st = type == OZ_F32 ? launch_planes<float>(mp, steps > 0, s) : type == OZ_BF16 ? launch_planes<__nv_bfloat16>(mp, steps > 0, s)
+                                                                                   : launch_planes<__half>(mp, steps > 0, s);
+    if (st != OZ_OK) return st;
     if (steps == 0) return OZ_OK;
 
     NewtonParams p{};
@@ -584,27 +704,28 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     p.otype = otype;
     p.transposed = mp.transposed;
     p.arrived = mp.arrived;
-    // blocks of 64 an accumulator: error of the result (16 x 512 x 2048, 1024 x 1024) 0.8e-6 and 0.7e-6 with one, 1.4e-6 and 1.2e-6 with two, 5.6e-6
-    // and 3.8e-6 with eight, where a rounding to 16 bits is 1.7e-3 (bfloat16) or 2e-4; the FP32 iteration in one precision has 2e-6 to 5e-6
-    p.core.seg = otype == OZ_F32 ? 2 : 8;
+    // Blocks of 64 an accumulator: error of the result (16 x 512 x 2048, 1024 x 1024) 0.8e-6 and 0.7e-6 with one, 1.4e-6 and 1.2e-6 with two, 5.6e-6
+    // and 3.8e-6 with eight, where a rounding to 16 bits is 1.7e-3 (bfloat16) or 2e-4; the FP32 iteration in one precision has 2e-6 to 5e-6.
+    // a X through P's diagonal is cut off with the sums (1024 x 1024, two blocks: 1.2e-6 -> 3.0e-6) but needs no second reading of X: 245 -> 191 us.
+    p.core.seg = otype == OZ_F32 ? 1 : 8;
     p.core.idesc = idesc16(false, 2);
     p.core.status = mp.status;
     for (int step = 0; step < steps; ++step) {
         const double sx = plane_scale(bound[step]), ss = plane_scale(bound[step] * bound[step]),
-                     sp = plane_scale(largest_polynomial(b, c, bound[step] * bound[step])),
+                     sp = plane_scale(largest_polynomial(folded ? a : 0.0, b, c, bound[step] * bound[step])),
                      next = step == steps - 1 ? 1.0 : plane_scale(bound[step + 1]);
-        float *alpha = p.alpha + 3 * step, *beta = p.beta + 3 * step;
-        alpha[kGram] = static_cast<float>(ss / (sx * sx));
-        alpha[kPolynomial] = static_cast<float>(sp * c / (ss * ss));
-        beta[kPolynomial] = static_cast<float>(sp * b / ss);
-        alpha[kApply] = static_cast<float>(next / (sp * sx));
-        beta[kApply] = static_cast<float>(next * a / sx);
+        p.alpha[3 * step + kGram] = static_cast<float>(ss / (sx * sx));
+        p.alpha[3 * step + kPolynomial] = static_cast<float>(sp * c / (ss * ss));
+        p.beta[3 * step + kPolynomial] = static_cast<float>(sp * b / ss);
+        p.diagonal[step] = folded ? static_cast<float>(sp * a) : 0.0f;
+        p.alpha[3 * step + kApply] = static_cast<float>(next / (sp * sx));
+        p.beta[3 * step + kApply] = static_cast<float>(next * a / sx);
     }
     // cycles of a block of 64 inner indices: the tensor cores' 1536 with 256 columns, shared memory's with fewer
     const int64_t wide = step_cycles<256>(p, 1536), half = step_cycles<128>(p, 960), narrow = step_cycles<64>(p, 790);
-    if (wide <= half && wide <= narrow) return launch_newton<256>(maps, p, s);
-    if (half <= narrow) return launch_newton<128>(maps, p, s);
-    return launch_newton<64>(maps, p, s);
+    if (wide <= half && wide <= narrow) return folded ? launch_newton<true, 256>(maps, p, s) : launch_newton<false, 256>(maps, p, s);
+    if (half <= narrow) return folded ? launch_newton<true, 128>(maps, p, s) : launch_newton<false, 128>(maps, p, s);
+    return folded ? launch_newton<true, 64>(maps, p, s) : launch_newton<false, 64>(maps, p, s);
 }
 
 }  // extern "C"

@@ -56,7 +56,7 @@ struct Ring16 {
     static constexpr int STAGE = PLANES * (A_PLANE + B_PLANE);
     static constexpr int STAGES = P16_RING_BYTES / STAGE;
     static constexpr int COLS = BN / 4;                                      // columns of an epilogue warp
-    static_assert(24 * STAGES + 40 <= P16_BARRIER_BYTES, "barriers");
+    static_assert(24 * STAGES + 48 <= P16_BARRIER_BYTES, "barriers");
 };
 
 // what the roles need to know of a launch and of a tile, whatever the policy
@@ -148,7 +148,7 @@ __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap
 //   P::RAGGED_K            k_begin and k_len are any numbers, and what lies behind them must not enter (MN-major operands only)
 //   P::setup(p, width, table)   all threads, after the predecessor's end: what `table`, shared memory of the launch's choice, holds
 //   P::phases(p)           products that follow one another in the launch, each of results of the one before
-//   P::ready(p, phase, abort_flag)   before a role's first access to what the phase before wrote; false: give up
+//   P::ready(p, phase, abort_flag)   the copying warp, before its first access to what the phase before wrote; false: give up
 //   P::done(p, phase)      the epilogue warps, after their last store of a phase
 //   P::total<CG, BN>(p, table, phase)   number of tiles
 //   P::decode<CG, BN>(p, table, phase, item)
@@ -175,9 +175,10 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
     const uint32_t tail_bar = empty_bar + 8 * STAGES;
     const uint32_t tfull_bar = tail_bar + 8 * STAGES;           // 2 x 8
     const uint32_t tempty_bar = tfull_bar + 16;                 // 2 x 8
+    const uint32_t go_bar = tempty_bar + 16;                    // 8: a phase may be read
     unsigned char *gen = smem_raw + (ring - raw) + P16_RING_BYTES;
-    volatile uint32_t *tmem_base_ptr = reinterpret_cast<volatile uint32_t *>(gen + 24 * STAGES + 32);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 24 * STAGES + 36);
+    volatile uint32_t *tmem_base_ptr = reinterpret_cast<volatile uint32_t *>(gen + 24 * STAGES + 40);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(gen + 24 * STAGES + 44);
     int *table = reinterpret_cast<int *>(gen + P16_BARRIER_BYTES);
     const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
 
@@ -193,17 +194,18 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             mbar_init(tfull_bar + 8 * s, 1);
             mbar_init(tempty_bar + 8 * s, P16_EPI_WARPS * CG);
         }
+        mbar_init(go_bar, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    dependency_wait();
+    if (!P::COOPERATIVE) dependency_wait();
     if (warp == 1) tmem_alloc<CG>(smem_u32(const_cast<uint32_t *>(tmem_base_ptr)), TMEM_COLUMNS);
     P::setup(p, BN, table);
     tc_fence_before();
     __syncthreads();
     if (CG * SPLIT > 1) cluster_sync_all();   // the peers' barriers exist before anything signals them
     tc_fence_after();
-    dependency_release();
+    if (!P::COOPERATIVE) dependency_release();
     const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_base_ptr, 0);
     unsigned int *const status = p.core.status;
     auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
@@ -221,7 +223,12 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
         if (warp == 0) {
             // -------------------------------------------------------- copies
             for (int ph = 0, phases = P::phases(p); ok && ph < phases; ++ph) {
-            ok = P::ready(p, ph, abort_flag);
+            if (ph > 0) {
+                // one warp of a block asks for the others' arrival: all of them asking keep the arrivals from getting through
+                ok = P::ready(p, ph, abort_flag);
+                if (!ok) break;
+                if (leader) mbar_arrive(go_bar);
+            }
             const CUtensorMap *mapA = P::map_a(maps, ph), *mapB = P::map_b(maps, ph);
             const int64_t total = P::template total<CG, BN>(p, table, ph);
             for (int64_t item = first_item; ok && item < total; item += item_step) {
@@ -406,7 +413,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             // (a warp that has given up goes through the phases all the same: done() is where the warps of a block meet)
             bool ok = true;
             for (int ph = 0, phases = P::phases(p); ph < phases; ++ph) {
-                ok = ok && P::ready(p, ph, abort_flag);
+                if (ph > 0) ok = ok && wait(go_bar, (ph & 1) ^ 1);
                 const int64_t total = P::template total<CG, BN>(p, table, ph);
                 for (int64_t item = first_item; ok && item < total; item += item_step) {
                     const typename P::Tile t = P::template decode<CG, BN>(p, table, ph, item);
@@ -516,7 +523,7 @@ oz_status_t launch_product16(const typename P::Maps &maps, const typename P::Par
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     if (P::COOPERATIVE) {
-        // blocks that wait for one another are on the device together
+        // blocks that wait for one another are on the device together; an ordinary link in the stream, to both sides
         attr[1].id = cudaLaunchAttributeCooperative;
         attr[1].val.cooperative = 1;
     } else {
