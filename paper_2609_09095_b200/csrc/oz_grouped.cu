@@ -287,7 +287,7 @@ struct GroupedPolicy {
             g = group_of(before, p.groups, static_cast<int>(item / tiles_m));
             const uint32_t in = item - static_cast<uint32_t>(before[g]) * tiles_m, tiles_n = static_cast<uint32_t>(before[g + 1] - before[g]);
             const int len = table[g + 1] - table[g], nt = static_cast<int>(in % tiles_n);
-            const int width = ((len + static_cast<int>(tiles_n) - 1) / static_cast<int>(tiles_n) + 16 * CG - 1) / (16 * CG) * (16 * CG);
+            const int width = ((len + static_cast<int>(tiles_n) - 1) / static_cast<int>(tiles_n) + 15) / 16 * 16;
             i0 = static_cast<int>(in / tiles_n) * 128 * CG;
             j0 = table[g] + nt * width;
             t.valid = min(width, table[g + 1] - j0);
@@ -300,7 +300,7 @@ struct GroupedPolicy {
         }
         t.a_row = i0;
         t.rows = static_cast<int>(p.m) - i0;
-        t.cols = (t.valid + 16 * CG - 1) / (16 * CG) * (16 * CG);
+        t.cols = (t.valid + 15) / 16 * 16;
         return t;
     }
 
@@ -329,6 +329,40 @@ int64_t most_tiles(const GroupedParams &p, int cg, int bn)
     return tiles_m * (full + some);
 }
 
+// Tiles for grouped columns: those whose rounds over the multiprocessors take least.  A block of 64 inner indices costs what it moves from L2
+// to shared memory, 51 to 62 bytes a cycle (pairs of 256 columns: the tensor cores, at the power cap); measured on 8 groups, 8192 columns,
+// 4096 x 4096: 680, 510, 450 and 400 cycles with 256, 128, 64 and 32 columns.  A group ends in half a tile in the mean.
+//   us, columns 256 / 128 / 64 / 32:  8 groups, 8192 columns, 4096 x 4096  199 / 289 / 489 / 853;  64 groups, 8192, 512 x 1024  19.6 / 22.8 / 28.8 / 40.9;
+//   16 groups, 1024, 2048 x 1024  15.8 / 13.8 / 17.9 / 25.9;  16 groups, 512, 1024 x 2048  13.9 / 12.3 / 11.8 / 19.5;  8 groups, 16, 2048 x 2048
+//   17.9 / 17.5 / 16.2 / 13.0.
+// Tiles of 32 columns that leave most multiprocessors idle are shared by 2 or 4 along the inner dimension (one column, 4096 x 4096: 17.9 / 12.8 /
+// 9.8 us with 1 / 2 / 4), where each has four blocks.
+struct TileShape {
+    int cg, bn, split;
+};
+TileShape tile_shape(const GroupedParams &p)
+{
+    constexpr struct {
+        int cg, bn, cycles;
+    } kinds[] = {{2, 256, 680}, {1, 128, 510}, {1, 64, 450}, {1, 32, 400}};
+    const int64_t sms = sm_count(), some = p.n < p.groups ? p.n : p.groups, blocks = (p.k + 63) / 64;
+    TileShape best{};
+    int64_t least = INT64_MAX;
+    for (const auto &kind : kinds) {
+        const int64_t tiles_n = p.n / kind.bn + some / 2 > some ? p.n / kind.bn + some / 2 : some;
+        const int64_t tiles = (p.m + 128 * kind.cg - 1) / (128 * kind.cg) * tiles_n, each = sms / kind.cg;
+        const int64_t cost = (tiles + each - 1) / each * kind.cycles;
+        if (cost < least) {
+            least = cost;
+            best = {kind.cg, kind.bn, 1};
+        }
+    }
+    if (best.bn == 32)
+        for (int split = 4; split > 1 && best.split == 1; split /= 2)
+            if (most_tiles<false>(p, 1, 32) * split <= sms && blocks >= 4 * split) best.split = split;
+    return best;
+}
+
 // The tensor-core form, where the operands' addresses and strides allow bulk copies; *taken says whether it did
 template <bool INNER>
 oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStream_t stream)
@@ -343,25 +377,26 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
     p.a_mn = p.rowA == 1 && p.innerA != 1;
     p.core.status = p.status;
     // sums that become 16-bit numbers need no segments
-    p.core.seg = p.ctype == OZ_F32 ? 4 : 1 << 24;
-    // Few columns a group: tiles as narrow, which leave the ring to the rows of A.
-    const int64_t mean = INNER ? p.n : p.n / p.groups;
-    const bool pairs = INNER || mean > 64;
-    const int bn = pairs ? 256 : mean > 32 ? 64 : 32;
+    p.core.seg = p.ctype == OZ_F32 ? 8 : 1 << 24;
+    const TileShape shape = INNER ? TileShape{2, 256, 1} : tile_shape(p);
     typename GroupedPolicy<INNER>::Maps maps;
     const int64_t za = p.shared_a ? 1 : p.groups;
-    const int boxB = bn == 32 ? 32 : 64;
+    const int boxB = shape.bn < 64 ? shape.bn : 64;
     if (!(p.a_mn ? make_map16(&maps.a, bf16, p.A, p.m, inner, lda, za, za > 1 ? p.strideA : lda, 64)
                       : make_map16(&maps.a, bf16, p.A, inner, p.m, lda, za, za > 1 ? p.strideA : lda, 64)) ||
         !(INNER ? make_map16(&maps.b, bf16, p.B, p.n, inner, ldb, 1, ldb, boxB) : make_map16(&maps.b, bf16, p.B, inner, p.n, ldb, 1, ldb, boxB)))
         return OZ_OK;
     *taken = true;
-    if (pairs) return launch_tiles<INNER, 2, 256>(p, bf16, maps, most_tiles<INNER>(p, 2, 256), stream);
+    const int64_t most = most_tiles<INNER>(p, shape.cg, shape.bn);
     if constexpr (!INNER) {
-        if (bn == 64) return launch_tiles<INNER, 1, 64>(p, bf16, maps, most_tiles<INNER>(p, 1, 64), stream);
-        return launch_tiles<INNER, 1, 32>(p, bf16, maps, most_tiles<INNER>(p, 1, 32), stream);
+        if (shape.bn == 128) return launch_tiles<INNER, 1, 128>(p, bf16, maps, most, stream);
+        if (shape.bn == 64) return launch_tiles<INNER, 1, 64>(p, bf16, maps, most, stream);
+        if (shape.bn == 32)
+            return shape.split == 4   ? launch_tiles<INNER, 1, 32, 4>(p, bf16, maps, most, stream)
+                   : shape.split == 2 ? launch_tiles<INNER, 1, 32, 2>(p, bf16, maps, most, stream)
+                                      : launch_tiles<INNER, 1, 32>(p, bf16, maps, most, stream);
     }
-    return OZ_OK;
+    return launch_tiles<INNER, 2, 256>(p, bf16, maps, most, stream);
 }
 
 // ---------------------------------------------------------------- checks that both entry points share

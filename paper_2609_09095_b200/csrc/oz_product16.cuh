@@ -352,12 +352,12 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
                 const int from = t.k_len & 63, to = (from + 15) & ~15;
                 const int boxes = 2 + (t.cols / CG + 63) / 64;
                 static_assert(!P::RAGGED_K || (PLANES == 1 && R::B_BOX_ROWS == 64), "ragged inner dimension: one plane, whole boxes");
-                const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
                 // a row of a box is one inner index: its eight chunks of 16 bytes stay in the row under the swizzle
-                for (int e = lane; e < boxes * (to - from) * 8; e += 32) {
-                    const int chunk = e & 7, row = from + (e >> 3) % (to - from), box = (e >> 3) / (to - from);
-                    *reinterpret_cast<uint4 *>(smem_raw + (ring - raw) + last * R::STAGE + box * P16_BOX_BYTES + row * 128 + chunk * 16) = zero;
-                }
+                unsigned char *first = smem_raw + (ring - raw) + last * R::STAGE + (from + lane / 8) * 128 + lane % 8 * 16;
+                for (int box = 0; box < boxes; ++box)
+#pragma unroll
+                    for (int row = 0; row < 16; row += 4)
+                        if (from + lane / 8 + row < to) *reinterpret_cast<uint4 *>(first + box * P16_BOX_BYTES + row * 128) = make_uint4(0u, 0u, 0u, 0u);
                 asm volatile("fence.proxy.async;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) {
