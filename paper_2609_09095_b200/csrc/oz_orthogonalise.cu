@@ -15,11 +15,12 @@
 // X keeps its r rows consecutive: for X X^T it is an operand stored along its rows, for P X one stored along the inner dimension,
 // both by the same bulk copies.  S and P are symmetric and computed on and below the diagonal only (see NewtonPolicy).
 //
-// Launches: sum of squares, planes of X, all products.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
+// Launches: sum of squares, planes of X, all products; narrow matrices: one.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
 // three times that on the pipe.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <type_traits>
@@ -31,7 +32,7 @@ namespace {
 
 constexpr int kMaxSteps = 100;
 constexpr int NORM_THREADS = 256;
-constexpr int MAX_PARTS = 296;                     // partial sums of squares of a matrix
+constexpr int MAX_PARTS = 192;                     // partial sums of squares of a matrix
 constexpr int PLANE_TILE = 64;
 constexpr unsigned long long kPhaseLimitNs = 4000000000ull;        // wait for the other blocks
 
@@ -137,22 +138,28 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_kernel(const MatrixParams p
     }
 }
 
-// 1 / (|G|_F + eps) times `scale`, as two factors; 0 for a matrix of zeros; NaN, which the whole update then is, for one that holds Inf or
-// NaN.  The first is a power of two, so that a product with both is rounded once, and neither the number nor what it passes through leaves the
-// range of FP32, from the smallest numbers to the largest.  One warp.
+// 1 / (|G|_F + eps) times `scale` from the sum of squares, as two factors; 0 for a matrix of zeros; NaN, which the whole update then is, for
+// one that holds Inf or NaN.  The first is a power of two, so that a product with both is rounded once, and neither the number nor what it passes
+// through leaves the range of FP32, from the smallest numbers to the largest.
+__device__ float2 norm_factor(double sum, double eps, double scale, unsigned int *status)
+{
+    if (!(sum <= 1.7e308)) {
+        atomicOr(status, 1u << OZ_ERR_NONFINITE_INPUT);
+        return make_float2(nanf(""), 1.0f);
+    }
+    if (sum == 0.0) return make_float2(0.0f, 0.0f);
+    const double f = scale / (sqrt(sum) + eps);
+    const int half = ilogb(f) / 2;
+    return make_float2(ldexpf(1.0f, half), static_cast<float>(ldexp(f, -half)));
+}
+
+// the same from a matrix' partial sums; one warp
 __device__ float2 inverse_norm(const MatrixParams &p, int64_t matrix, double scale)
 {
     double sum = 0.0;
     for (int i = threadIdx.x % 32; i < p.parts; i += 32) sum += p.sums[matrix * p.parts + i];
     for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-    if (!(sum <= 1.7e308)) {
-        atomicOr(p.status, 1u << OZ_ERR_NONFINITE_INPUT);
-        return make_float2(nanf(""), 1.0f);
-    }
-    if (sum == 0.0) return make_float2(0.0f, 0.0f);
-    const double f = scale / (sqrt(sum) + p.eps);
-    const int half = ilogb(f) / 2;
-    return make_float2(ldexpf(1.0f, half), static_cast<float>(ldexp(f, -half)));
+    return norm_factor(sum, p.eps, scale, p.status);
 }
 
 // Planes of X, tiles of 64 x 64; a lane has two consecutive rows, a warp eight columns.  Through shared memory where X is the transpose of
@@ -533,6 +540,348 @@ int64_t step_cycles(const NewtonParams &p, int each)
     return sum;
 }
 
+// ---------------------------------------------------------------- narrow matrices
+// r <= 128 and c <= 2048: a cluster of up to 8 CTAs keeps a matrix in shared memory through all steps, each CTA up to 256 of its
+// columns, and one launch does everything, the norm included.  A step:
+//   S   every CTA multiplies its columns, X X^T; the partial sums go to the CTA that owns a column of S, which adds them in the order
+//       of the CTAs and gives its planes to all
+//   P   every CTA by itself: 128 x 128 x 128
+//   X   every CTA its own columns, in place: the products read all of X before the first element is written
+// hi hi and the sum of the mixed products have accumulators of their own, three of hi hi in turn, added in FP32.
+// Bound: latencies, about 3 us a product (launches or meetings of the whole device take 6).
+constexpr int SMALL_R = 128, SMALL_W = 256, SMALL_CTAS = 8, SMALL_THREADS = 512;
+constexpr int SMALL_LINES_BYTES = SMALL_R * 128;                         // a plane of 64 elements of S or P
+
+struct SmallParams {
+    MatrixParams m;
+    int steps, width;               // columns of a CTA, a multiple of 16
+    float alpha[3 * kMaxSteps], beta[3 * kMaxSteps];
+};
+
+// byte of element i of a line, its chunk of 64 elements apart: the 128-byte swizzle of a line of 128 bytes
+__device__ __forceinline__ uint32_t swizzled(int line, int i) { return static_cast<uint32_t>(line * 128 + ((((i & 63) >> 3) ^ (line & 7)) << 4) + (i & 7) * 2); }
+
+__device__ __forceinline__ uint64_t small_desc(uint32_t addr, uint32_t leading)
+{
+    return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(leading >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
+           (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+}
+
+template <class T, int CTAS>
+__global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __grid_constant__ SmallParams p)
+{
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ double sums[SMALL_CTAS + SMALL_THREADS / 32];
+    __shared__ __align__(8) unsigned long long bar_word;
+    __shared__ uint32_t tmem_word;
+    __shared__ int abort_word;
+    const MatrixParams &m = p.m;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+    const uint32_t place = CTAS > 1 ? cluster_ctarank() : 0u;
+    const int64_t matrix = blockIdx.x / CTAS;
+    const int W = p.width, r16 = (m.r + 15) / 16 * 16;
+    const int first = static_cast<int>(place) * W, mine = max(0, min(W, m.c - first));            // the CTA's columns of X
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    unsigned char *const X = smem_raw + (base - raw);                      // [hi, lo][chunk][W lines][128 bytes]
+    const uint32_t chunk_x = static_cast<uint32_t>(W) * 128, plane_x = 2 * chunk_x;
+    unsigned char *const S = X + 2 * plane_x;                              // [hi, lo][chunk][128 lines][128 bytes]
+    constexpr uint32_t chunk_s = SMALL_LINES_BYTES, plane_s = 2 * chunk_s;
+    const uint32_t x_addr = base, s_addr = base + 2 * plane_x, bar = smem_u32(&bar_word);
+    volatile int *abort_flag = &abort_word;
+
+    if (tid == 0) {
+        mbar_init(bar, 1);
+        abort_word = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    dependency_wait();
+    if (warp == 0) tmem_alloc<1>(smem_u32(&tmem_word), 512);
+
+    // ---- norm: sums of squares of the CTA's columns, then of the matrix
+    const T *G = static_cast<const T *>(m.G) + matrix * m.strideG;
+    const int64_t step_i = m.transposed ? m.ldg : 1, step_j = m.transposed ? 1 : m.ldg;
+    // element e of the CTA's part, along the direction in which G is consecutive
+    auto place_of = [&](int e, int &i, int &j) {
+        if (m.transposed) {
+            i = e / mine;
+            j = e - i * mine;
+        } else {
+            j = e / m.r;
+            i = e - j * m.r;
+        }
+    };
+    const int elements = mine * m.r;
+    double sum = 0.0;
+#pragma unroll 4
+    for (int e = tid; e < elements; e += SMALL_THREADS) {
+        int i, j;
+        place_of(e, i, j);
+        const double v = to_float(G[i * step_i + (first + j) * step_j]);
+        sum = fma(v, v, sum);
+    }
+    for (int d = 16; d > 0; d /= 2) sum += __shfl_down_sync(0xFFFFFFFFu, sum, d);
+    if (lane == 0) sums[SMALL_CTAS + warp] = sum;
+    // columns and rows that X does not have are zeros
+    for (uint32_t at = tid * 16; at < 2 * plane_x; at += SMALL_THREADS * 16) *reinterpret_cast<uint4 *>(X + at) = make_uint4(0u, 0u, 0u, 0u);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    dependency_release();
+    const uint32_t tmem = tmem_word;
+    auto meet = [&] {
+        __syncwarp();
+        cluster_sync_all();
+    };
+    if (CTAS > 1) meet();                       // the others' shared memory may be written
+    if (tid == 0) {
+        double all = 0.0;
+        for (int w = 0; w < SMALL_THREADS / 32; ++w) all += sums[SMALL_CTAS + w];
+        for (uint32_t to = 0; to < CTAS; ++to)
+            asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(map_to_cta(smem_u32(&sums[place]), to)), "d"(all) : "memory");
+    }
+    if (CTAS > 1) meet();
+    else __syncthreads();
+    sum = 0.0;
+    for (int w = 0; w < CTAS; ++w) sum += sums[w];
+    const float2 f = norm_factor(sum, m.eps, static_cast<double>(m.scale), m.status);
+
+    // ---- planes
+#pragma unroll 4
+    for (int e = tid; e < elements; e += SMALL_THREADS) {
+        int i, j;
+        place_of(e, i, j);
+        __half hi, lo;
+        split_planes(to_float(G[i * step_i + (first + j) * step_j]) * f.x * f.y, &hi, &lo);
+        unsigned char *to = X + (i >> 6) * chunk_x + swizzled(j, i);
+        *reinterpret_cast<__half *>(to) = hi;
+        *reinterpret_cast<__half *>(to + plane_x) = lo;
+    }
+    asm volatile("fence.proxy.async;" ::: "memory");
+    __syncthreads();
+
+    const int q = warp & 3, part = warp >> 2, row = q * 32 + lane;         // TMEM lanes of the warp, its quarter of the columns
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(q * 32) << 16);
+    const bool leader = warp == 0 && elect_one();
+    uint32_t phase = 0;
+    // Accumulators side by side: those of hi hi, which take the pieces of the inner dimension in turn, then the mixed products'.
+    // (Of 64 x 1000 in FP32 the error against 64 bits is 3.5e-6 with one of hi hi.)
+    // D = A B over pieces of 16 inner indices; a plane's descriptor of piece k is its first one + k % 4 inner + k / 4 outer
+    struct Operand {
+        uint64_t first;
+        uint32_t plane, inner, outer;
+    };
+    auto product = [&](uint32_t idesc, int pieces, int cols, const Operand &a, const Operand &b) {
+        const uint32_t hh = cols <= 128 ? 3 : 1, wide = cols <= 128 ? 128 : 256, mixed = tmem + hh * wide;
+        if (warp == 0) {
+            // (the whole warp walks: descriptors stay in uniform registers)
+            tc_fence_after();
+            const uint32_t id = idesc | (static_cast<uint32_t>(cols >> 3) << 17);
+            uint32_t turn = 0;
+            for (int k = 0; k < pieces; ++k) {
+                const uint64_t da = a.first + (k & 3) * a.inner + (k >> 2) * a.outer, db = b.first + (k & 3) * b.inner + (k >> 2) * b.outer;
+                if (leader) {
+                    umma16<1>(mixed, da + a.plane, db, id, k > 0);
+                    umma16<1>(mixed, da, db + b.plane, id, 1u);
+                    umma16<1>(tmem + turn * wide, da, db, id, k >= static_cast<int>(hh));
+                }
+                turn = turn + 1 == hh ? 0 : turn + 1;
+            }
+            if (leader) umma_commit<1>(bar);
+        }
+        __syncwarp();
+        mbar_wait(bar, phase, abort_flag, m.status);
+        __syncwarp();
+        phase ^= 1u;
+        tc_fence_after();
+    };
+    // after the epilogue of a product: its accumulators may be overwritten, what it stored may be multiplied
+    auto finished = [&] {
+        tc_fence_before();
+        asm volatile("fence.proxy.async;" ::: "memory");
+        __syncthreads();
+    };
+    // sixteen columns of a product of `cols` columns over `pieces` pieces
+    auto add = [&](int col, int cols, int pieces, float (&v)[16]) {
+        const int hh = cols <= 128 ? 3 : 1, wide = cols <= 128 ? 128 : 256;
+        uint32_t a[16];
+        tmem_ld16(lanes + hh * wide + col, a);
+#pragma unroll
+        for (int c = 0; c < 16; ++c) v[c] = __uint_as_float(a[c]);
+        for (int h = min(hh, pieces) - 1; h >= 0; --h) {
+            tmem_ld16(lanes + h * wide + col, a);
+#pragma unroll
+            for (int c = 0; c < 16; ++c) v[c] += __uint_as_float(a[c]);
+        }
+    };
+    const uint32_t desc_base = idesc16(false, 1);
+    const Operand x_rows{small_desc(x_addr, chunk_x), plane_x >> 4, 2048 >> 4, 4 * 2048 >> 4},     // along the rows, for X X^T
+        x_lines{small_desc(x_addr, 16), plane_x >> 4, 32 >> 4, chunk_x >> 4}, s_lines{small_desc(s_addr, 16), plane_s >> 4, 32 >> 4, chunk_s >> 4};
+    // the others have read what this CTA is going to overwrite in their S: said as soon as P has been multiplied, asked before the first store
+    auto may_overwrite = [&] {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    };
+    if (CTAS > 1) may_overwrite();
+
+    for (int step = 0; step < p.steps; ++step) {
+        const float *alpha = p.alpha + 3 * step, *beta = p.beta + 3 * step;
+        // ---- S
+        const int pieces = (mine + 15) / 16;
+        product(desc_base | (3u << 15), pieces, r16, x_rows, x_rows);
+        if constexpr (CTAS == 1) {
+#pragma unroll 1
+            for (int c0 = part * 16; c0 < r16; c0 += 64) {
+                float v[16];
+                add(c0, r16, pieces, v);
+                if (row < r16)
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        __half hi, lo;
+                        split_planes(v[c] * alpha[kGram], &hi, &lo);
+                        unsigned char *to = S + (row >> 6) * chunk_s + swizzled(c0 + c, row);
+                        *reinterpret_cast<__half *>(to) = hi;
+                        *reinterpret_cast<__half *>(to + plane_s) = lo;
+                    }
+            }
+        } else {
+            constexpr int OWN = SMALL_R / CTAS;                            // columns of S that a CTA owns; boxes [sender][column][row] in its S
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+#pragma unroll 1
+            for (int c0 = part * 16; c0 < r16; c0 += 64) {
+                float v[16];
+                if (mine > 0) {
+                    add(c0, r16, pieces, v);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) v[c] = 0.0f;
+                }
+                // (16 columns have one owner)
+                const uint32_t to = map_to_cta(s_addr + static_cast<uint32_t>(((place * OWN + c0 % OWN) * SMALL_R + row) * 4), static_cast<uint32_t>(c0 / OWN));
+                static_assert(OWN % 16 == 0, "owner of a piece");
+                if (row < r16)
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) store_cluster(to + c * SMALL_R * 4, v[c]);
+            }
+            meet();
+            // two rows a thread
+            constexpr int EACH = OWN / 8;
+            const int own_row = 2 * (tid % 64), own_col = tid / 64;
+            float2 total[EACH];
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                total[e] = make_float2(0.0f, 0.0f);
+                for (int s = 0; s < CTAS; ++s) {
+                    const float2 v = *reinterpret_cast<const float2 *>(S + ((s * OWN + own_col + 8 * e) * SMALL_R + own_row) * 4);
+                    total[e].x += v.x;
+                    total[e].y += v.y;
+                }
+            }
+            meet();                                                        // every sum is in registers: S may be written
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const int j = static_cast<int>(place) * OWN + own_col + 8 * e;
+                if (j < r16 && own_row < r16) {
+                    __half2 hi, lo;
+                    split_planes(total[e].x * alpha[kGram], &hi.x, &lo.x);
+                    split_planes(total[e].y * alpha[kGram], &hi.y, &lo.y);
+                    const uint32_t to = s_addr + (own_row >> 6) * chunk_s + swizzled(j, own_row);
+                    for (uint32_t cta = 0; cta < CTAS; ++cta) {
+                        store_cluster(map_to_cta(to, cta), *reinterpret_cast<const float *>(&hi));
+                        store_cluster(map_to_cta(to + plane_s, cta), *reinterpret_cast<const float *>(&lo));
+                    }
+                }
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");
+            meet();
+        }
+        finished();
+        // ---- P
+        product(desc_base, r16 / 16, r16, s_lines, s_lines);
+#pragma unroll 1
+        for (int c0 = part * 16; c0 < r16; c0 += 64) {
+            float v[16];
+            add(c0, r16, r16 / 16, v);
+            if (row < r16)
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    unsigned char *at = S + (row >> 6) * chunk_s + swizzled(c0 + c, row);
+                    __half *hi = reinterpret_cast<__half *>(at), *lo = reinterpret_cast<__half *>(at + plane_s);
+                    split_planes(fmaf(beta[kPolynomial], __half2float(*hi) + __half2float(*lo), alpha[kPolynomial] * v[c]), hi, lo);
+                }
+        }
+        finished();
+        // ---- X
+        const int cols = 16 * pieces;
+        const bool last = step == p.steps - 1;
+        if (mine == 0 && CTAS > 1) may_overwrite();
+        if (mine > 0) {
+            product(desc_base, r16 / 16, cols, s_lines, x_lines);
+            if (CTAS > 1) may_overwrite();
+#pragma unroll 1
+            for (int c0 = part * 16; c0 < cols; c0 += 64) {
+                float v[16];
+                add(c0, cols, r16 / 16, v);
+                if (row < r16)
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        unsigned char *at = X + (row >> 6) * chunk_x + swizzled(c0 + c, row);
+                        __half *hi = reinterpret_cast<__half *>(at), *lo = reinterpret_cast<__half *>(at + plane_x);
+                        v[c] = fmaf(beta[kApply], __half2float(*hi) + __half2float(*lo), alpha[kApply] * v[c]);
+                        if (!last) split_planes(v[c], hi, lo);
+                    }
+                if (last && row < m.r) {
+                    const int64_t at = matrix * m.strideO + row * (m.transposed ? m.ldo : 1), by = m.transposed ? 1 : m.ldo;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        if (c0 + c < mine) store_number(m.O, at + (first + c0 + c) * by, v[c], m.otype);
+                }
+            }
+        }
+        finished();
+    }
+    if (CTAS > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (CTAS > 1) meet();                                                  // no CTA leaves while another may still write to it
+    if (warp == 0) tmem_dealloc<1>(tmem, 512);
+}
+
+template <class T, int CTAS>
+oz_status_t launch_small(const SmallParams &p, cudaStream_t stream)
+{
+    auto kernel = newton_small_kernel<T, CTAS>;
+    const size_t smem = 1024 + 4 * static_cast<size_t>(p.width) * 128 + 4 * SMALL_LINES_BYTES;
+    static std::atomic<unsigned long long> ready{0};
+    OZ_CUDA_CHECK(allow_shared(kernel, 1024 + 4 * SMALL_W * 128 + 4 * SMALL_LINES_BYTES, ready));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.m.count * CTAS));
+    cfg.blockDim = dim3(SMALL_THREADS);
+    // (more than half of a multiprocessor's: two CTAs that want all of its tensor memory never share it)
+    cfg.dynamicSmemBytes = smem > 120 * 1024 ? smem : 120 * 1024;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CTAS;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    OZ_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, p));
+    count_launch();
+    return OZ_OK;
+}
+
+template <class T>
+oz_status_t launch_small(const SmallParams &p, int ctas, cudaStream_t stream)
+{
+    switch (ctas) {
+        case 1: return launch_small<T, 1>(p, stream);
+        case 2: return launch_small<T, 2>(p, stream);
+        case 4: return launch_small<T, 4>(p, stream);
+        default: return launch_small<T, 8>(p, stream);
+    }
+}
+
 // ---------------------------------------------------------------- host side
 struct Layout {
     int64_t r, c, chunks;
@@ -546,7 +895,7 @@ Layout layout_of(int64_t m, int64_t n, int64_t count)
     l.r = m < n ? m : n;
     l.c = m < n ? n : m;
     l.chunks = (l.r + 63) / 64;
-    // pieces of 16 elements a thread, two blocks a multiprocessor in all
+    // pieces of 16 elements a thread, about a block a multiprocessor in all
     const int64_t pieces = (m * n + NORM_THREADS * 16 - 1) / (NORM_THREADS * 16), share = (MAX_PARTS + count - 1) / count;
     l.parts = static_cast<int>(pieces < share ? pieces : share);
     size_t at = 0;
@@ -654,11 +1003,6 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     char *ws = static_cast<char *>(workspace);
     __half *x[2] = {reinterpret_cast<__half *>(ws + l.x[0]), reinterpret_cast<__half *>(ws + l.x[1])};
     __half *gram = reinterpret_cast<__half *>(ws + l.s), *poly = reinterpret_cast<__half *>(ws + l.poly);
-    NewtonMaps maps;
-    if (steps && !(make_pair_map16(&maps.x[0], x[0], l.chunks, l.c, count) && make_pair_map16(&maps.x[1], x[1], l.chunks, l.c, count) &&
-                   make_pair_map16(&maps.gram, gram, l.chunks, l.r, count) && make_pair_map16(&maps.poly, poly, l.chunks, l.r, count)))
-        return OZ_ERR_CUDA;
-
     MatrixParams mp{};
     mp.m = m;
     mp.n = n;
@@ -682,6 +1026,39 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     mp.scale = static_cast<float>(plane_scale(bound[0]));
     mp.X = x[0];
     mp.status = device_status_word();
+    // of each phase: result = alpha accumulator + beta S or beta X, in the scales of the planes
+    float alpha[3 * kMaxSteps], beta[3 * kMaxSteps], diagonal[kMaxSteps];
+    const bool small = steps > 0 && l.r <= SMALL_R && l.c <= SMALL_W * SMALL_CTAS;
+    for (int step = 0; step < steps; ++step) {
+        const double sx = plane_scale(bound[step]), ss = plane_scale(bound[step] * bound[step]),
+                     sp = plane_scale(largest_polynomial(folded && !small ? a : 0.0, b, c, bound[step] * bound[step])),
+                     next = step == steps - 1 ? 1.0 : plane_scale(bound[step + 1]);
+        alpha[3 * step + kGram] = static_cast<float>(ss / (sx * sx));
+        beta[3 * step + kGram] = 0.0f;
+        alpha[3 * step + kPolynomial] = static_cast<float>(sp * c / (ss * ss));
+        beta[3 * step + kPolynomial] = static_cast<float>(sp * b / ss);
+        diagonal[step] = folded ? static_cast<float>(sp * a) : 0.0f;
+        alpha[3 * step + kApply] = static_cast<float>(next / (sp * sx));
+        beta[3 * step + kApply] = static_cast<float>(next * a / sx);
+    }
+    if (small) {
+        SmallParams sp{};
+        sp.m = mp;
+        sp.steps = steps;
+        std::copy(alpha, alpha + 3 * steps, sp.alpha);
+        std::copy(beta, beta + 3 * steps, sp.beta);
+        // CTAs of 128 columns while all matrices together find room on the device, of 256 at most
+        int ctas = 1;
+        while (ctas < SMALL_CTAS && (l.c > SMALL_W * ctas || (l.c > 128 * ctas && 2 * ctas * count <= sm_count()))) ctas *= 2;
+        sp.width = static_cast<int>(round_up((l.c + ctas - 1) / ctas, 16));
+        if (count * ctas > 0x7FFFFFFF) return OZ_ERR_UNSUPPORTED;
+        return type == OZ_F32 ? launch_small<float>(sp, ctas, s) : type == OZ_BF16 ? launch_small<__nv_bfloat16>(sp, ctas, s) : launch_small<__half>(sp, ctas, s);
+    }
+    NewtonMaps maps;
+    if (steps && !(make_pair_map16(&maps.x[0], x[0], l.chunks, l.c, count) && make_pair_map16(&maps.x[1], x[1], l.chunks, l.c, count) &&
+                   make_pair_map16(&maps.gram, gram, l.chunks, l.r, count) && make_pair_map16(&maps.poly, poly, l.chunks, l.r, count)))
+        return OZ_ERR_CUDA;
+
     if (count * l.parts > 0x7FFFFFFF) return OZ_ERR_UNSUPPORTED;
     st = type == OZ_F32 ? launch_planes<float>(mp, steps > 0, s) : type == OZ_BF16 ? launch_planes<__nv_bfloat16>(mp, steps > 0, s)
                                                                                    : launch_planes<__half>(mp, steps > 0, s);
@@ -710,17 +1087,9 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     p.core.seg = otype == OZ_F32 ? 1 : 8;
     p.core.idesc = idesc16(false, 2);
     p.core.status = mp.status;
-    for (int step = 0; step < steps; ++step) {
-        const double sx = plane_scale(bound[step]), ss = plane_scale(bound[step] * bound[step]),
-                     sp = plane_scale(largest_polynomial(folded ? a : 0.0, b, c, bound[step] * bound[step])),
-                     next = step == steps - 1 ? 1.0 : plane_scale(bound[step + 1]);
-        p.alpha[3 * step + kGram] = static_cast<float>(ss / (sx * sx));
-        p.alpha[3 * step + kPolynomial] = static_cast<float>(sp * c / (ss * ss));
-        p.beta[3 * step + kPolynomial] = static_cast<float>(sp * b / ss);
-        p.diagonal[step] = folded ? static_cast<float>(sp * a) : 0.0f;
-        p.alpha[3 * step + kApply] = static_cast<float>(next / (sp * sx));
-        p.beta[3 * step + kApply] = static_cast<float>(next * a / sx);
-    }
+    std::copy(alpha, alpha + 3 * steps, p.alpha);
+    std::copy(beta, beta + 3 * steps, p.beta);
+    std::copy(diagonal, diagonal + steps, p.diagonal);
     // cycles of a block of 64 inner indices: the tensor cores' 1536 with 256 columns, shared memory's with fewer
     const int64_t wide = step_cycles<256>(p, 1536), half = step_cycles<128>(p, 960), narrow = step_cycles<64>(p, 790);
     if (wide <= half && wide <= narrow) return folded ? launch_newton<true, 256>(maps, p, s) : launch_newton<false, 256>(maps, p, s);

@@ -71,7 +71,7 @@ struct Tile16 {
     int cols;                   // columns computed: a multiple of 16 CG; of plane pairs, whose operand B may be along its rows, 64 or a multiple of 128
 };
 
-inline uint32_t idesc16(bool bf16, int cg)
+__host__ __device__ inline uint32_t idesc16(bool bf16, int cg)
 {
     const uint32_t fmt = bf16 ? 1u : 0u;
     return (1u << 4) | (fmt << 7) | (fmt << 10) | (static_cast<uint32_t>((128 * cg) >> 4) << 24);
