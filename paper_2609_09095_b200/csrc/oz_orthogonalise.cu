@@ -555,6 +555,7 @@ constexpr int SMALL_LINES_BYTES = SMALL_R * 128;                         // a pl
 struct SmallParams {
     MatrixParams m;
     int steps, width;               // columns of a CTA, a multiple of 16
+    int boxes_in_s;                 // no room for the partial sums beside S: two more meetings of the cluster a step
     float alpha[3 * kMaxSteps], beta[3 * kMaxSteps];
 };
 
@@ -586,7 +587,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
     const uint32_t chunk_x = static_cast<uint32_t>(W) * 128, plane_x = 2 * chunk_x;
     unsigned char *const S = X + 2 * plane_x;                              // [hi, lo][chunk][128 lines][128 bytes]
     constexpr uint32_t chunk_s = SMALL_LINES_BYTES, plane_s = 2 * chunk_s;
-    const uint32_t x_addr = base, s_addr = base + 2 * plane_x, bar = smem_u32(&bar_word);
+    const unsigned char *const boxes = p.boxes_in_s ? S : S + 2 * plane_s;
+    const uint32_t x_addr = base, s_addr = base + 2 * plane_x, box_addr = s_addr + (p.boxes_in_s ? 0u : 2 * plane_s), bar = smem_u32(&bar_word);
     volatile int *abort_flag = &abort_word;
 
     if (tid == 0) {
@@ -600,25 +602,28 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
     // ---- norm: sums of squares of the CTA's columns, then of the matrix
     const T *G = static_cast<const T *>(m.G) + matrix * m.strideG;
     const int64_t step_i = m.transposed ? m.ldg : 1, step_j = m.transposed ? 1 : m.ldg;
-    // element e of the CTA's part, along the direction in which G is consecutive
-    auto place_of = [&](int e, int &i, int &j) {
-        if (m.transposed) {
-            i = e / mine;
-            j = e - i * mine;
-        } else {
-            j = e / m.r;
-            i = e - j * m.r;
-        }
+    // the CTA's part line by line along the direction in which G is consecutive: a warp a line, eight elements of a lane (two lines' four) at a time
+    const int lines = m.transposed ? m.r : mine, inner = m.transposed ? mine : m.r;
+    const int64_t step_line = m.transposed ? step_i : step_j;
+    const T *part_of_g = G + first * step_j;
+    auto each_element = [&](auto use) {
+        for (int l0 = warp; l0 < lines; l0 += 2 * (SMALL_THREADS / 32))
+            for (int e0 = lane; e0 < inner; e0 += 128) {
+                float v[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int l = l0 + u / 4 * (SMALL_THREADS / 32), e = e0 + u % 4 * 32;
+                    v[u] = l < lines && e < inner ? to_float(part_of_g[l * step_line + e]) : 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int l = l0 + u / 4 * (SMALL_THREADS / 32), e = e0 + u % 4 * 32;
+                    if (l < lines && e < inner) use(m.transposed ? l : e, m.transposed ? e : l, v[u]);
+                }
+            }
     };
-    const int elements = mine * m.r;
     double sum = 0.0;
-#pragma unroll 4
-    for (int e = tid; e < elements; e += SMALL_THREADS) {
-        int i, j;
-        place_of(e, i, j);
-        const double v = to_float(G[i * step_i + (first + j) * step_j]);
-        sum = fma(v, v, sum);
-    }
+    each_element([&](int, int, float v) { sum = fma(static_cast<double>(v), static_cast<double>(v), sum); });
     for (int d = 16; d > 0; d /= 2) sum += __shfl_down_sync(0xFFFFFFFFu, sum, d);
     if (lane == 0) sums[SMALL_CTAS + warp] = sum;
     // columns and rows that X does not have are zeros
@@ -646,16 +651,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
     const float2 f = norm_factor(sum, m.eps, static_cast<double>(m.scale), m.status);
 
     // ---- planes
-#pragma unroll 4
-    for (int e = tid; e < elements; e += SMALL_THREADS) {
-        int i, j;
-        place_of(e, i, j);
+    each_element([&](int i, int j, float v) {
         __half hi, lo;
-        split_planes(to_float(G[i * step_i + (first + j) * step_j]) * f.x * f.y, &hi, &lo);
+        split_planes(v * f.x * f.y, &hi, &lo);
         unsigned char *to = X + (i >> 6) * chunk_x + swizzled(j, i);
         *reinterpret_cast<__half *>(to) = hi;
         *reinterpret_cast<__half *>(to + plane_x) = lo;
-    }
+    });
     asm volatile("fence.proxy.async;" ::: "memory");
     __syncthreads();
 
@@ -716,12 +718,21 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
     const uint32_t desc_base = idesc16(false, 1);
     const Operand x_rows{small_desc(x_addr, chunk_x), plane_x >> 4, 2048 >> 4, 4 * 2048 >> 4},     // along the rows, for X X^T
         x_lines{small_desc(x_addr, 16), plane_x >> 4, 32 >> 4, chunk_x >> 4}, s_lines{small_desc(s_addr, 16), plane_s >> 4, 32 >> 4, chunk_s >> 4};
-    // the others have read what this CTA is going to overwrite in their S: said as soon as P has been multiplied, asked before the first store
-    auto may_overwrite = [&] {
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    // the thread's row of sixteen lines of plane pairs
+    auto read_pairs = [&](const unsigned char *chunk, uint32_t plane, int line, float (&v)[16]) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            const unsigned char *at = chunk + swizzled(line + c, row);
+            v[c] = __half2float(*reinterpret_cast<const __half *>(at)) + __half2float(*reinterpret_cast<const __half *>(at + plane));
+        }
     };
-    if (CTAS > 1) may_overwrite();
+    auto write_pairs = [&](unsigned char *chunk, uint32_t plane, int line, const float (&v)[16]) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            unsigned char *at = chunk + swizzled(line + c, row);
+            split_planes(v[c], reinterpret_cast<__half *>(at), reinterpret_cast<__half *>(at + plane));
+        }
+    };
 
     for (int step = 0; step < p.steps; ++step) {
         const float *alpha = p.alpha + 3 * step, *beta = p.beta + 3 * step;
@@ -733,19 +744,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
             for (int c0 = part * 16; c0 < r16; c0 += 64) {
                 float v[16];
                 add(c0, r16, pieces, v);
-                if (row < r16)
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        __half hi, lo;
-                        split_planes(v[c] * alpha[kGram], &hi, &lo);
-                        unsigned char *to = S + (row >> 6) * chunk_s + swizzled(c0 + c, row);
-                        *reinterpret_cast<__half *>(to) = hi;
-                        *reinterpret_cast<__half *>(to + plane_s) = lo;
-                    }
+                for (int c = 0; c < 16; ++c) v[c] *= alpha[kGram];
+                if (row < r16) write_pairs(S + (row >> 6) * chunk_s, plane_s, c0, v);
             }
         } else {
-            constexpr int OWN = SMALL_R / CTAS;                            // columns of S that a CTA owns; boxes [sender][column][row] in its S
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            constexpr int OWN = SMALL_R / CTAS;                            // columns of S that a CTA owns; boxes [sender][column][row]
+            if (p.boxes_in_s) meet();                                      // nobody multiplies with P any more
 #pragma unroll 1
             for (int c0 = part * 16; c0 < r16; c0 += 64) {
                 float v[16];
@@ -756,7 +761,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
                     for (int c = 0; c < 16; ++c) v[c] = 0.0f;
                 }
                 // (16 columns have one owner)
-                const uint32_t to = map_to_cta(s_addr + static_cast<uint32_t>(((place * OWN + c0 % OWN) * SMALL_R + row) * 4), static_cast<uint32_t>(c0 / OWN));
+                const uint32_t to = map_to_cta(box_addr + static_cast<uint32_t>(((place * OWN + c0 % OWN) * SMALL_R + row) * 4), static_cast<uint32_t>(c0 / OWN));
                 static_assert(OWN % 16 == 0, "owner of a piece");
                 if (row < r16)
 #pragma unroll
@@ -771,12 +776,12 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
             for (int e = 0; e < EACH; ++e) {
                 total[e] = make_float2(0.0f, 0.0f);
                 for (int s = 0; s < CTAS; ++s) {
-                    const float2 v = *reinterpret_cast<const float2 *>(S + ((s * OWN + own_col + 8 * e) * SMALL_R + own_row) * 4);
+                    const float2 v = *reinterpret_cast<const float2 *>(boxes + ((s * OWN + own_col + 8 * e) * SMALL_R + own_row) * 4);
                     total[e].x += v.x;
                     total[e].y += v.y;
                 }
             }
-            meet();                                                        // every sum is in registers: S may be written
+            if (p.boxes_in_s) meet();                                      // every sum is in registers: S may be written
 #pragma unroll
             for (int e = 0; e < EACH; ++e) {
                 const int j = static_cast<int>(place) * OWN + own_col + 8 * e;
@@ -799,47 +804,55 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) newton_small_kernel(const __
         product(desc_base, r16 / 16, r16, s_lines, s_lines);
 #pragma unroll 1
         for (int c0 = part * 16; c0 < r16; c0 += 64) {
-            float v[16];
+            float v[16], was[16];
+            read_pairs(S + (row >> 6) * chunk_s, plane_s, c0, was);
             add(c0, r16, r16 / 16, v);
-            if (row < r16)
 #pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    unsigned char *at = S + (row >> 6) * chunk_s + swizzled(c0 + c, row);
-                    __half *hi = reinterpret_cast<__half *>(at), *lo = reinterpret_cast<__half *>(at + plane_s);
-                    split_planes(fmaf(beta[kPolynomial], __half2float(*hi) + __half2float(*lo), alpha[kPolynomial] * v[c]), hi, lo);
-                }
+            for (int c = 0; c < 16; ++c) v[c] = fmaf(beta[kPolynomial], was[c], alpha[kPolynomial] * v[c]);
+            if (row < r16) write_pairs(S + (row >> 6) * chunk_s, plane_s, c0, v);
         }
         finished();
         // ---- X
         const int cols = 16 * pieces;
         const bool last = step == p.steps - 1;
-        if (mine == 0 && CTAS > 1) may_overwrite();
         if (mine > 0) {
             product(desc_base, r16 / 16, cols, s_lines, x_lines);
-            if (CTAS > 1) may_overwrite();
 #pragma unroll 1
             for (int c0 = part * 16; c0 < cols; c0 += 64) {
-                float v[16];
+                float v[16], was[16];
+                unsigned char *x = X + (row >> 6) * chunk_x;
+                read_pairs(x, plane_x, c0, was);
                 add(c0, cols, r16 / 16, v);
-                if (row < r16)
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        unsigned char *at = X + (row >> 6) * chunk_x + swizzled(c0 + c, row);
-                        __half *hi = reinterpret_cast<__half *>(at), *lo = reinterpret_cast<__half *>(at + plane_x);
-                        v[c] = fmaf(beta[kApply], __half2float(*hi) + __half2float(*lo), alpha[kApply] * v[c]);
-                        if (!last) split_planes(v[c], hi, lo);
-                    }
-                if (last && row < m.r) {
-                    const int64_t at = matrix * m.strideO + row * (m.transposed ? m.ldo : 1), by = m.transposed ? 1 : m.ldo;
+                for (int c = 0; c < 16; ++c) v[c] = fmaf(beta[kApply], was[c], alpha[kApply] * v[c]);
+                if (!last) {
+                    if (row < r16) write_pairs(x, plane_x, c0, v);
+                } else if (row < m.r) {
+                    auto as = [&](auto *O) {
+                        using Out = typename std::remove_pointer<decltype(O)>::type;
+                        O += matrix * m.strideO + (m.transposed ? row * m.ldo + first + c0 : row + (first + c0) * m.ldo);
+                        if (m.transposed && c0 + 16 <= mine && reinterpret_cast<uintptr_t>(O) % 16 == 0) {
+                            // (one number at a time, a warp's 32 rows are 32 places in memory with every store)
+                            __align__(16) Out w[16];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c)
-                        if (c0 + c < mine) store_number(m.O, at + (first + c0 + c) * by, v[c], m.otype);
+                            for (int c = 0; c < 16; ++c) w[c] = from_float<Out>(v[c]);
+#pragma unroll
+                            for (int c = 0; c < static_cast<int>(sizeof(Out)); ++c) reinterpret_cast<uint4 *>(O)[c] = reinterpret_cast<const uint4 *>(w)[c];
+                        } else {
+                            const int64_t by = m.transposed ? 1 : m.ldo;
+#pragma unroll
+                            for (int c = 0; c < 16; ++c)
+                                if (c0 + c < mine) O[c * by] = from_float<Out>(v[c]);
+                        }
+                    };
+                    if (m.otype == OZ_F32) as(static_cast<float *>(m.O));
+                    else if (m.otype == OZ_BF16) as(static_cast<__nv_bfloat16 *>(m.O));
+                    else as(static_cast<__half *>(m.O));
                 }
             }
         }
         finished();
     }
-    if (CTAS > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (CTAS > 1) meet();                                                  // no CTA leaves while another may still write to it
     if (warp == 0) tmem_dealloc<1>(tmem, 512);
 }
@@ -848,9 +861,10 @@ template <class T, int CTAS>
 oz_status_t launch_small(const SmallParams &p, cudaStream_t stream)
 {
     auto kernel = newton_small_kernel<T, CTAS>;
-    const size_t smem = 1024 + 4 * static_cast<size_t>(p.width) * 128 + 4 * SMALL_LINES_BYTES;
+    const size_t smem = 1024 + 4 * static_cast<size_t>(p.width) * 128 + (CTAS == 1 || p.boxes_in_s ? 4 : 8) * SMALL_LINES_BYTES;
     static std::atomic<unsigned long long> ready{0};
     OZ_CUDA_CHECK(allow_shared(kernel, 1024 + 4 * SMALL_W * 128 + 4 * SMALL_LINES_BYTES, ready));
+    static_assert(4 * 128 * 128 + 8 * SMALL_LINES_BYTES <= 4 * SMALL_W * 128 + 4 * SMALL_LINES_BYTES, "boxes of their own with up to 128 columns");
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.m.count * CTAS));
     cfg.blockDim = dim3(SMALL_THREADS);
@@ -1051,6 +1065,7 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
         int ctas = 1;
         while (ctas < SMALL_CTAS && (l.c > SMALL_W * ctas || (l.c > 128 * ctas && 2 * ctas * count <= sm_count()))) ctas *= 2;
         sp.width = static_cast<int>(round_up((l.c + ctas - 1) / ctas, 16));
+        sp.boxes_in_s = sp.width > 128;
         if (count * ctas > 0x7FFFFFFF) return OZ_ERR_UNSUPPORTED;
         return type == OZ_F32 ? launch_small<float>(sp, ctas, s) : type == OZ_BF16 ? launch_small<__nv_bfloat16>(sp, ctas, s) : launch_small<__half>(sp, ctas, s);
     }
