@@ -1067,7 +1067,7 @@ const char *oz_status_string(oz_status_t status)
     switch (status) {
         case OZ_OK: return "ok";
         case OZ_ERR_INVALID_ARG: return "invalid argument";
-        case OZ_ERR_UNSUPPORTED: return "unsupported (k above OZ_K_MAX, or alpha/beta not in {+-1}/{0,1})";
+        case OZ_ERR_UNSUPPORTED: return "unsupported (k above OZ_K_MAX, alpha/beta not in {+-1}/{0,1}, or beyond an entry point's limits)";
         case OZ_ERR_WORKSPACE: return "workspace missing or too small";
         case OZ_ERR_CUDA: return "CUDA call failed";
         case OZ_ERR_NONFINITE_INPUT: return "Inf/NaN in an operand";

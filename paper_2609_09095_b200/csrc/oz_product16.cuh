@@ -513,7 +513,6 @@ oz_status_t launch_product16(const typename P::Maps &maps, const typename P::Par
     int64_t groups = sm_count() / CG;
     if (SPLIT > 1 || most_tiles < groups) groups = most_tiles;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(groups * CG * SPLIT));
     cfg.blockDim = dim3(P16_THREADS);
     cfg.dynamicSmemBytes = P16_RING_BYTES + 1024 + P16_BARRIER_BYTES + table_bytes;
     cfg.stream = stream;
@@ -523,13 +522,28 @@ oz_status_t launch_product16(const typename P::Maps &maps, const typename P::Par
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
     if (P::COOPERATIVE) {
-        // blocks that wait for one another are on the device together; an ordinary link in the stream, to both sides
+        // blocks that wait for one another are on the device together: no more than it holds (asked once a device)
+        static std::atomic<int> held[64];
+        int dev = 0, most = 0;
+        OZ_CUDA_CHECK(cudaGetDevice(&dev));
+        most = held[dev & 63].load(std::memory_order_relaxed);
+        if (most == 0) {
+            cfg.gridDim = dim3(CG * SPLIT);
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            OZ_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&most, kernel, &cfg));
+            if (most <= 0) return OZ_ERR_CUDA;
+            held[dev & 63].store(most, std::memory_order_relaxed);
+        }
+        if (groups > most) groups = most;
+        // an ordinary link in the stream, to both sides
         attr[1].id = cudaLaunchAttributeCooperative;
         attr[1].val.cooperative = 1;
     } else {
         attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
         attr[1].val.programmaticStreamSerializationAllowed = 1;
     }
+    cfg.gridDim = dim3(static_cast<unsigned>(groups * CG * SPLIT));
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     OZ_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, maps, p));

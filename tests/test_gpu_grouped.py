@@ -280,3 +280,51 @@ def test_most_groups_and_beyond_32_bits():
     grad = run_wgrad(x, dy, offsets, torch.zeros(2, m, k, device="cuda"))
     a, b = dy[-60:].double(), x[-60:].double()
     within(grad[1], a.T @ b, a.abs().T @ b.abs(), 60)
+
+
+# sizes that the rule sends to each tile shape: 32 columns undivided and shared by 2 and 4, 64, 128, 256
+@pytest.mark.parametrize("sizes,m,k", [([1], 2048, 1024), ([1, 0, 1], 4096, 1032), ([2] * 40, 640, 520), ([0, 40, 24, 50], 1024, 256), ([60] * 16, 2048, 200),
+                                       ([1000, 900, 2000], 1304, 328)])
+@pytest.mark.parametrize("transA", [0, 1])
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32)])
+def test_tile_shapes(sizes, m, k, transA, dtype, out_dtype):
+    offsets = offsets_of(sizes, 1)
+    n = 1 + sum(sizes) + 2
+    x = tensor(n, k, dtype=dtype, seed=30)
+    w = tensor(len(sizes), *((m, k) if transA else (k, m)), dtype=dtype, seed=31, scale=k ** -0.5)
+    old = tensor(n, m, dtype=out_dtype, seed=32)
+    for beta in (0.0, 1.0):
+        check_grouped(x, w, offsets, run_grouped(x, w, offsets, old.clone(), transA, beta), old, transA, beta)
+    assert oz.oz_query_status() in (oz.OZ_OK, oz.OZ_ERR_RANGE)
+
+
+def test_long_sums_in_fp32():
+    """Sums of positive numbers, whose running value only grows: each of the K / 16 additions of the tensor core to it cuts off less than a unit in the
+    last place, 2^-23, of an accumulator that is started again every 512 indices and so holds at most 512 / K of the whole (and a unit more for a
+    sixteen's own sum); what is started again is added with rounding, 2^-24 of the whole each time."""
+    K = 8192
+    x, w = tensor(3, K, dtype=torch.bfloat16, seed=33).abs(), tensor(1, 256, K, dtype=torch.bfloat16, seed=34).abs()
+    y = run_grouped(x, w, offsets_of([3]), torch.zeros(3, 256, device="cuda"), 1)
+    exact = x.double() @ w[0].double().T
+    # numbers are alike enough that a piece's share of the sum is at most twice its share of the indices
+    steps = 512 // 16 + 17
+    tol = exact * (steps * 2.0 ** -23 + K // 512 * 2.0 ** -24)
+    assert ((y.double() - exact).abs() <= tol).all()
+    grad = run_wgrad(w[0].T.contiguous(), w[0].T.contiguous(), offsets_of([K]), torch.zeros(1, 256, 256, device="cuda"))[0]
+    exact = w[0].double() @ w[0].double().T
+    assert ((grad.double() - exact).abs() <= exact * (steps * 2.0 ** -23 + K // 512 * 2.0 ** -24)).all()
+
+
+def test_broadcast_inputs():
+    """One row of tokens for a whole group (stride 0 is expanded by the caller), the same expert twice, the same gradient for all tokens."""
+    m, k = 264, 136
+    offsets = offsets_of([100, 30])
+    x = tensor(1, k, dtype=torch.bfloat16, seed=35).expand(130, k).contiguous()
+    w = tensor(1, m, k, dtype=torch.bfloat16, seed=36, scale=0.1).expand(2, m, k)
+    y = run_grouped(x, w, offsets, torch.zeros(130, m, dtype=torch.float32, device="cuda"), 1)
+    assert torch.equal(y, y[:1].expand_as(y))
+    dy = torch.ones(130, m, dtype=torch.bfloat16, device="cuda")
+    grad = run_wgrad(x, dy, offsets, torch.zeros(2, m, k, device="cuda"))
+    for g, count in ((0, 100), (1, 30)):
+        exact = count * x[0].double()
+        assert ((grad[g].double() - exact).abs() <= (count + 1) * 2.0 ** -23 * exact.abs()).all()

@@ -249,3 +249,46 @@ def test_experts_step():
         else:
             exact = iterate(normalised(dw[g], 1e-7), 5, USUAL)
             assert (o[g].double() - exact).norm() <= m ** 0.5 * spread_bound(5, USUAL, 1.3) + exact.norm() * U24
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 128, 2048), (1, 2049, 128), (2, 20, 513), (3, 129, 256), (200, 100, 300), (150, 128, 129), (1, 3, 2048), (5, 17, 1100)])
+def test_narrow_and_its_borders(count, rows, cols):
+    """One launch in shared memory up to 128 x 2048 (513 columns leave the last block of a cluster without any), the general form next to it."""
+    g = tensor(count, rows, cols, seed=13)
+    got = update(g)
+    assert oz.oz_query_status() in (oz.OZ_OK, oz.OZ_ERR_RANGE)
+    for i in range(0, count, 37):
+        exact = iterate(normalised(g[i], 1e-7), 5, USUAL)
+        off = (got[i].double() - exact).norm()
+        assert off <= min(rows, cols) ** 0.5 * spread_bound(5, USUAL, 1.3) + exact.norm() * U24
+        assert off <= 4 * (iterate_f32(g[i]).double() - exact).norm() + 2 * exact.norm() * U24
+
+
+@pytest.mark.parametrize("rows,cols", [(300, 260), (260, 300), (700, 150)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_general_in_place_and_strided(rows, cols, dtype):
+    g = tensor(2, rows, cols, seed=14, dtype=dtype)
+    want = update(g, dtype)
+    same = g.clone()
+    assert torch.equal(update(same, out=same), want)
+    held = torch.full((2 * rows * (cols + 3) + 1,), 5.0, dtype=dtype, device="cuda")
+    out = held[1:].as_strided((2, rows, cols), (rows * (cols + 3), cols + 3, 1))
+    source = torch.zeros(2, rows + 2, cols + 5, dtype=dtype, device="cuda")
+    source[:, 1:1 + rows, 3:3 + cols] = g
+    got = update(source[:, 1:1 + rows, 3:3 + cols], out=out)
+    # the sum of squares is taken in another order there: the last bit of the norm may differ
+    exact = iterate(normalised(g[0], 1e-7), 5, USUAL)
+    assert (got[0].double() - want[0].double()).norm() <= 2 * min(rows, cols) ** 0.5 * spread_bound(5, USUAL, 1.3) + exact.norm() * torch.finfo(dtype).eps
+    mask = torch.ones_like(held, dtype=torch.bool)
+    mask[1:].as_strided((2, rows, cols), (rows * (cols + 3), cols + 3, 1))[:] = False
+    assert (held[mask] == 5.0).all()
+
+
+def test_one_matrix_for_all():
+    g = tensor(1, 200, 140, seed=15)
+    want = update(g)
+    shared = g[0].as_strided((3, 200, 140), (0, 140, 1))
+    got = update(shared)
+    for i in range(3):
+        assert (got[i].double() - want[0].double()).norm() <= 2 * 140 ** 0.5 * spread_bound(5, USUAL, 1.3)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
