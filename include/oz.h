@@ -13,6 +13,10 @@
  *   3. reconstruction (Algorithm 3, Eq. 4-5): CRT, lift to [-M/2, M/2), inverse scaling,
  *      one rounding to FP64.
  *
+ * Beside it stand products of 16-bit matrices grouped by ragged sizes, with their gradients, and an orthogonalised
+ * update by Newton-Schulz products, for layers of experts in language models (oz_gemm_grouped, oz_gemm_grouped_wgrad,
+ * oz_orthogonalise).
+ *
  * General conventions
  *   - Matrices are column-major, no transposes: A is m x k (lda >= m), B is k x n
  *     (ldb >= k), C is m x n (ldc >= m).

@@ -228,6 +228,10 @@ oz_status_t launch_plain(const GroupedParams &p, cudaStream_t stream)
 }
 
 // ---------------------------------------------------------------- tensor cores
+// Bound, large products: the tensor cores at the power cap (8192 columns, 4 groups, 4096 x 4096: 179 us, 1540 TFLOP/s, the library's product of the same
+// operations 180; tensor pipe 86 % active, operands read from memory once); few columns a group: memory (32 groups, 128 columns, 2048 x 4096:
+// 90 us, 6.0 TB/s); results of short sums: the stores, one a warp and column, five cycles each (32 weight gradients 1536 x 1024 of 32 tokens: 32 us
+// in 16 bits and 38 in FP32; neighbouring lanes exchanging numbers for four-byte stores: 37).
 // Rows of a tile are rows of C (features, whatever the group's size), its columns are those of a group (tokens) or of C_g: a group of
 // few tokens then takes an MMA of few columns, and consecutive lanes hold consecutive elements of the column-major result.
 // A group's columns are cut into equal tiles of at most BN.  The tiles that share rows of A follow one another, so that A comes from memory once.
@@ -376,8 +380,10 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
     const bool bf16 = type == OZ_BF16;
     p.a_mn = p.rowA == 1 && p.innerA != 1;
     p.core.status = p.status;
-    // sums that become 16-bit numbers need no segments
-    p.core.seg = p.ctype == OZ_F32 ? 8 : 1 << 24;
+    // Segments of 512 inner indices for FP32 results: error against 64 bits of the weight gradients of 16 experts, 16384 tokens, 4.4e-7, and 302 us; with
+    // segments of 256 2.3e-7 and 332 us (the epilogue, still storing the tile before, holds up the MMAs after two segments).  Of 4096 for 16-bit
+    // results, which keeps what is cut off, 2^-24 of the sum 256 times in the mean, a tenth of a half-precision rounding.
+    p.core.seg = p.ctype == OZ_F32 ? 8 : 64;
     const TileShape shape = INNER ? TileShape{2, 256, 1} : tile_shape(p);
     typename GroupedPolicy<INNER>::Maps maps;
     const int64_t za = p.shared_a ? 1 : p.groups;

@@ -16,7 +16,9 @@
 // both by the same bulk copies.  S and P are symmetric and computed on and below the diagonal only (see NewtonPolicy).
 //
 // Launches: sum of squares, planes of X, all products; narrow matrices: one.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
-// three times that on the pipe.
+// three times that on the pipe.  Five steps: 4096 x 4096 in FP32 3.7 ms, 1.1 PFLOP/s on the pipe (power cap; the FP32 iteration of a library 34);
+// 16 x 512 x 2048 603 us (gram on 48 of 74 pairs, 256 tiles of P X in 4 rounds); 1024 x 1024 168 us, 10 us a phase: 6.6 of them products, the rest
+// storing, meeting and the first copies.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -34,7 +36,7 @@ constexpr int kMaxSteps = 100;
 constexpr int NORM_THREADS = 256;
 constexpr int MAX_PARTS = 192;                     // partial sums of squares of a matrix
 constexpr int PLANE_TILE = 64;
-constexpr unsigned long long kPhaseLimitNs = 4000000000ull;        // wait for the other blocks
+constexpr unsigned long long kPhaseLimitNs = 4000000000ull;        // 4 s for the other blocks: twice what each of them waits for a barrier
 
 template <class T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -295,6 +297,7 @@ __host__ __device__ __forceinline__ uint32_t newton_tiles(int r, int c, int phas
     return wide * tm * (tm - 1) / 2 + (tm - 1) * wide + last;
 }
 
+// (One launch a product: 283 us for 1024 x 1024 where this takes 168.)
 // All steps in one launch: phase 3 s is S = X X^T of step s, 3 s + 1 P, 3 s + 2 the new X.  The blocks meet between the phases.
 // Tiles are 256 rows x BN columns by pairs: the three plane products of a block read shared memory at 106 bytes a cycle with BN = 256; those of
 // tiles of 128 x 128 by single CTAs would at 213 of the 128 that it has.
@@ -548,7 +551,8 @@ int64_t step_cycles(const NewtonParams &p, int each)
 //   P   every CTA by itself: 128 x 128 x 128
 //   X   every CTA its own columns, in place: the products read all of X before the first element is written
 // hi hi and the sum of the mixed products have accumulators of their own, three of hi hi in turn, added in FP32.
-// Bound: latencies, about 3 us a product (launches or meetings of the whole device take 6).
+// Bound: latencies and two-byte accesses of shared memory, 2 to 4 us a product (launches or meetings of the whole device: 6).  128 x 512 in FP32: 71 us
+// (the general form 107), 32 x 32: 20, 128 x 2048: 100 (general 177), 148 of 128 x 512: 193.
 constexpr int SMALL_R = 128, SMALL_W = 256, SMALL_CTAS = 8, SMALL_THREADS = 512;
 constexpr int SMALL_LINES_BYTES = SMALL_R * 128;                         // a plane of 64 elements of S or P
 
@@ -1105,7 +1109,8 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     std::copy(alpha, alpha + 3 * steps, p.alpha);
     std::copy(beta, beta + 3 * steps, p.beta);
     std::copy(diagonal, diagonal + steps, p.diagonal);
-    // cycles of a block of 64 inner indices: the tensor cores' 1536 with 256 columns, shared memory's with fewer
+    // Cycles of a block of 64 inner indices: the tensor cores' 1536 with 256 columns, shared memory's with fewer.  Columns 256 / 128 / 64 in us: 1024 x 1024
+    // 375 / 247 / 256, 3 x 1009 x 517 326 / 302 / 281, 16 x 512 x 2048 764 / 720 / 841, 4096 x 4096 3593 / 3519 / 5062 (all before blocks asked once).
     const int64_t wide = step_cycles<256>(p, 1536), half = step_cycles<128>(p, 960), narrow = step_cycles<64>(p, 790);
     if (wide <= half && wide <= narrow) return folded ? launch_newton<true, 256>(maps, p, s) : launch_newton<false, 256>(maps, p, s);
     if (half <= narrow) return folded ? launch_newton<true, 128>(maps, p, s) : launch_newton<false, 128>(maps, p, s);

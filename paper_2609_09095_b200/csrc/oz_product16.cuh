@@ -29,7 +29,7 @@
 // Every wait is bounded: when one runs out the CTA reports OZ_ERR_TIMEOUT, leaves its loops, frees its tensor memory and returns.
 //
 // The tensor memory is taken after dependency_wait() and the successor let in after that: a CTA that waits for its predecessor
-// holds none of what the predecessor still has to take.
+// holds none of what the predecessor still has to take.  (Cooperative launches neither wait nor let in.)
 #pragma once
 
 #include "oz_tcgen05.cuh"
