@@ -11,6 +11,7 @@
 
 #include <atomic>
 #include <type_traits>
+#include <utility>
 
 #include "oz_product16.cuh"
 
@@ -127,6 +128,39 @@ __device__ __forceinline__ void store_row_of(T *c, int64_t ldc, const float (&ac
     }
 }
 
+// c[(row + i) ldc + col + j] = the j-th number of lane i, of rows below `rows` and columns below `valid`; one warp
+template <class T, int N>
+__device__ __forceinline__ void store_rows(T *c, int64_t ldc, const float (&acc)[N], int row, int rows, int col, int valid, unsigned char *staging)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < N / 8; ++k) {
+        __align__(16) T v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = from_float<T>(acc[8 * k + e]);
+        *reinterpret_cast<uint4 *>(staging + lane * 128 + ((k ^ (lane & 7)) << 4)) = *reinterpret_cast<const uint4 *>(v);
+    }
+    __syncwarp();
+    const int chunk = lane & 7, j = col + 8 * chunk;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+        const int i = 4 * s + lane / 8;
+        const uint4 v = *reinterpret_cast<const uint4 *>(staging + i * 128 + ((chunk ^ (i & 7)) << 4));
+        if (row + i < rows) {
+            T *to = c + (row + i) * ldc + j;
+            if (j + 8 <= valid) {
+                *reinterpret_cast<uint4 *>(to) = v;
+            } else {
+                const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (j + e < valid) reinterpret_cast<uint16_t *>(to)[e] = static_cast<uint16_t>(words[e / 2] >> (16 * (e & 1)));
+            }
+        }
+    }
+    __syncwarp();
+}
+
 // (Type and old value are told apart once a row: inside the loop that took 36 instructions an element, and 8 us a tile of 256 x 256.)
 template <int N>
 __device__ __forceinline__ void store_row(void *C, int64_t at, int64_t ldc, const float (&acc)[N], int valid, int ctype, int accumulate)
@@ -230,22 +264,27 @@ oz_status_t launch_plain(const GroupedParams &p, cudaStream_t stream)
 // ---------------------------------------------------------------- tensor cores
 // Bound, large products: the tensor cores at the power cap (8192 columns, 4 groups, 4096 x 4096: 179 us, 1540 TFLOP/s, the library's product of the same
 // operations 180; tensor pipe 86 % active, operands read from memory once); few columns a group: memory (32 groups, 128 columns, 2048 x 4096:
-// 90 us, 6.0 TB/s); results of short sums: the stores, one a warp and column, five cycles each (32 weight gradients 1536 x 1024 of 32 tokens: 32 us
-// in 16 bits and 38 in FP32; neighbouring lanes exchanging numbers for four-byte stores: 37).
+// 90 us, 6.0 TB/s); results of short sums: the stores, five cycles a warp's store of a column (32 weight gradients 1536 x 1024 of 32 tokens: 38 us in
+// FP32; in 16 bits 31, with neighbouring lanes exchanging numbers for four-byte stores 37, by rows 25).
 // Rows of a tile are rows of C (features, whatever the group's size), its columns are those of a group (tokens) or of C_g: a group of
 // few tokens then takes an MMA of few columns, and consecutive lanes hold consecutive elements of the column-major result.
 // A group's columns are cut into equal tiles of at most BN.  The tiles that share rows of A follow one another, so that A comes from memory once.
-template <bool INNER>
+struct GroupedMaps {
+    CUtensorMap a, b;
+};
+
+// ROWS: a thread's results are consecutive elements of C instead (the operands of an inner grouped product exchanged: its rows are the columns of C), 16-bit
+// numbers, 16-byte aligned.  A warp turns its 32 x 64 through shared memory and stores 128 bytes of four rows at a time.
+template <bool INNER, bool ROWS = false>
 struct GroupedPolicy {
     using Params = GroupedParams;
     struct Tile : Tile16 {
         int rows, valid;            // rows of C from the tile's first on, columns that belong to the group
         int64_t c;                  // element of C at the tile's first row and column
     };
-    struct Maps {
-        CUtensorMap a, b;
-    };
+    using Maps = GroupedMaps;
     static constexpr bool RAGGED_K = INNER, COOPERATIVE = false;
+    static constexpr int STAGING = ROWS ? P16_EPI_WARPS * 32 * 128 : 0;
     static __device__ __forceinline__ const CUtensorMap *map_a(const Maps &m, int) { return &m.a; }
     static __device__ __forceinline__ const CUtensorMap *map_b(const Maps &m, int) { return &m.b; }
     static __device__ __forceinline__ int phases(const Params &) { return 1; }
@@ -285,7 +324,7 @@ struct GroupedPolicy {
             t.k_len = table[g + 1] - table[g];
             t.a_z = t.b_z = 0;
             t.b_row = j0;
-            t.c = g * p.strideC + i0 + j0 * p.ldc;
+            t.c = g * p.strideC + (ROWS ? j0 + i0 * p.ldc : i0 + j0 * p.ldc);
         } else {
             const int *before = table + p.groups + 1;
             g = group_of(before, p.groups, static_cast<int>(item / tiles_m));
@@ -309,18 +348,24 @@ struct GroupedPolicy {
     }
 
     template <int CG, int BN, int N>
-    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col)
+    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col, unsigned char *staging)
     {
+        if constexpr (ROWS) {
+            static_assert(!ROWS || N == 64, "128 bytes a row");
+            if (p.ctype == OZ_BF16) store_rows(static_cast<__nv_bfloat16 *>(p.C) + t.c, p.ldc, acc, row & ~31, t.rows, col, t.valid, staging);
+            else store_rows(static_cast<__half *>(p.C) + t.c, p.ldc, acc, row & ~31, t.rows, col, t.valid, staging);
+            return;
+        }
         if (row >= t.rows || (t.k_len == 0 && p.accumulate)) return;
         store_row(p.C, t.c + row + col * p.ldc, p.ldc, acc, t.valid - col, p.ctype, p.accumulate);
     }
 };
 
-template <bool INNER, int CG, int BN, int SPLIT = 1>
-oz_status_t launch_tiles(GroupedParams &p, bool bf16, const typename GroupedPolicy<INNER>::Maps &maps, int64_t most, cudaStream_t stream)
+template <bool INNER, int CG, int BN, int SPLIT = 1, bool ROWS = false>
+oz_status_t launch_tiles(GroupedParams &p, bool bf16, const GroupedMaps &maps, int64_t most, cudaStream_t stream)
 {
     p.core.idesc = idesc16(bf16, CG);
-    return launch_product16<GroupedPolicy<INNER>, CG, BN, 1, SPLIT>(maps, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
+    return launch_product16<GroupedPolicy<INNER, ROWS>, CG, BN, 1, SPLIT>(maps, p, most, 2 * (p.groups + 1) * sizeof(int), stream);
 }
 
 // tiles of 128 cg x bn at most: what the host knows of the groups is their number and that of all columns
@@ -369,9 +414,20 @@ TileShape tile_shape(const GroupedParams &p)
 
 // The tensor-core form, where the operands' addresses and strides allow bulk copies; *taken says whether it did
 template <bool INNER>
-oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStream_t stream)
+oz_status_t launch_tensor(GroupedParams p, oz_type_t type, bool *taken, cudaStream_t stream)
 {
     *taken = false;
+    bool by_rows = false;
+    if constexpr (INNER) {
+        // Of short sums, whose stores count more than the two stages of the ring that they take (bfloat16, numbers one by one -> by rows: 32 groups of 32,
+        // 1536 x 1024, 30.7 -> 25.1 us; 16 of 256, 1024 x 2048, 24.8 -> 23.2; 16 of 512, 2048 x 2048, 62.7 -> 67.9; 16 of 1024, 4096 x 2048, 204 -> 215).
+        by_rows = p.columns <= 256ll * p.groups && p.ctype != OZ_F32 && !p.accumulate && p.ldc % 8 == 0 && p.strideC % 8 == 0 && reinterpret_cast<uintptr_t>(p.C) % 16 == 0;
+        if (by_rows) {
+            std::swap(p.A, p.B);
+            std::swap(p.m, p.n);
+            std::swap(p.innerA, p.innerB);
+        }
+    }
     const int64_t inner = INNER ? p.columns : p.k, lda = p.rowA == 1 ? p.innerA : p.rowA, ldb = p.colB == 1 ? p.innerB : p.colB;
     if (inner == 0 || most_tiles<INNER>(p, 1, 32) >= (1ll << 31)) return OZ_OK;
     p.shared_a = INNER || p.strideA == 0 || p.groups == 1;
@@ -385,7 +441,7 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
     // results, which keeps what is cut off, 2^-24 of the sum 256 times in the mean, a tenth of a half-precision rounding.
     p.core.seg = p.ctype == OZ_F32 ? 8 : 64;
     const TileShape shape = INNER ? TileShape{2, 256, 1} : tile_shape(p);
-    typename GroupedPolicy<INNER>::Maps maps;
+    GroupedMaps maps;
     const int64_t za = p.shared_a ? 1 : p.groups;
     const int boxB = shape.bn < 64 ? shape.bn : 64;
     if (!(p.a_mn ? make_map16(&maps.a, bf16, p.A, p.m, inner, lda, za, za > 1 ? p.strideA : lda, 64)
@@ -402,6 +458,8 @@ oz_status_t launch_tensor(GroupedParams &p, oz_type_t type, bool *taken, cudaStr
                    : shape.split == 2 ? launch_tiles<INNER, 1, 32, 2>(p, bf16, maps, most, stream)
                                       : launch_tiles<INNER, 1, 32>(p, bf16, maps, most, stream);
     }
+    if constexpr (INNER)
+        if (by_rows) return launch_tiles<true, 2, 256, 1, true>(p, bf16, maps, most, stream);
     return launch_tiles<INNER, 2, 256>(p, bf16, maps, most, stream);
 }
 

@@ -313,6 +313,7 @@ struct NewtonPolicy {
         int matrix, phase;
     };
     static constexpr bool RAGGED_K = false, COOPERATIVE = true;
+    static constexpr int STAGING = 0;
 
     static __device__ __forceinline__ const CUtensorMap *map_a(const Maps &m, int phase)
     {
@@ -416,7 +417,7 @@ struct NewtonPolicy {
 
     // A thread has one row of X, S or P (consecutive lanes consecutive rows) and N columns, eight at a time.
     template <int CG, int BN, int N>
-    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col)
+    static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col, unsigned char *)
     {
         const int left = (t.phase % 3 == kApply ? p.c : p.r) - t.b_row - col;
         if (left >= N) store_columns<true>(p, t, acc, t.a_row + row, t.b_row + col, left);

@@ -44,7 +44,7 @@ constexpr int P16_BOX_BYTES = 64 * 128;
 constexpr int P16_RING_BYTES = 192 * 1024;
 constexpr int P16_BARRIER_BYTES = 512;
 
-template <int CG, int BN, int PLANES>
+template <int CG, int BN, int PLANES, int STAGING>
 struct Ring16 {
     static_assert(P16_EPI_WARPS * 4 * 32 * (BN / 4) <= P16_RING_BYTES, "sums of the other members of a cluster");
     static constexpr int B_ROWS = BN / CG;                                   // columns of the tile that one CTA loads
@@ -54,7 +54,7 @@ struct Ring16 {
     static constexpr int A_PLANE = 2 * P16_BOX_BYTES;
     static constexpr int B_PLANE = B_BOXES * B_BOX_BYTES;
     static constexpr int STAGE = PLANES * (A_PLANE + B_PLANE);
-    static constexpr int STAGES = P16_RING_BYTES / STAGE;
+    static constexpr int STAGES = (P16_RING_BYTES - STAGING) / STAGE;
     static constexpr int COLS = BN / 4;                                      // columns of an epilogue warp
     static_assert(24 * STAGES + 48 <= P16_BARRIER_BYTES, "barriers");
 };
@@ -153,13 +153,15 @@ __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap
 //   P::total<CG, BN>(p, table, phase)   number of tiles
 //   P::decode<CG, BN>(p, table, phase, item)
 //   P::a_mn(p, tile, block), P::b_mn(p, tile, block): whether the operand of the tile's block is stored along its rows (MN-major)
+//   P::STAGING             bytes of shared memory, off the ring, through which store() takes its results: a sixteenth an epilogue warp
 //   P::COOPERATIVE         the launch's blocks wait for one another (between phases)
-//   P::store<CG, BN>(p, tile, acc, row, col): the thread's results, row of the tile (0 .. 128 CG - 1), as many columns from col on as acc holds
+//   P::store<CG, BN>(p, tile, acc, row, col, staging): the thread's results, row of the tile (0 .. 128 CG - 1), as many columns from col on as acc
+//                          holds; called by whole warps
 template <class P, int CG, int BN, int PLANES, int SPLIT>
 __global__ void __launch_bounds__(P16_THREADS, 1)
 product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_constant__ typename P::Params p)
 {
-    using R = Ring16<CG, BN, PLANES>;
+    using R = Ring16<CG, BN, PLANES, P::STAGING>;
     constexpr int STAGES = R::STAGES;
     constexpr int TMEM_COLUMNS = 2 * BN < 32 ? 32 : 2 * BN;
     const uint32_t place = CG * SPLIT > 1 ? cluster_ctarank() : 0u;
@@ -376,6 +378,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
     constexpr int W = R::COLS < 16 ? 8 : 16;                 // columns of a load: the running sums and these stay within the registers
     const int q = warp & 3;                                  // lane quarter of the tensor memory
     const int part = (warp - P16_FIRST_EPI) >> 2;            // BN / 4 of the tile's columns
+    unsigned char *const staging = smem_raw + (ring - raw) + (P16_RING_BYTES - P::STAGING) + (warp - P16_FIRST_EPI) * (P::STAGING / P16_EPI_WARPS);
     float acc[R::COLS];
     // the tile's sums (of the member's blocks)
     int slot = 0;
@@ -418,7 +421,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
                 for (int64_t item = first_item; ok && item < total; item += item_step) {
                     const typename P::Tile t = P::template decode<CG, BN>(p, table, ph, item);
                     ok = collect(t);
-                    if (ok) P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS);
+                    if (ok) P::template store<CG, BN>(p, t, acc, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS, staging);
                 }
                 P::done(p, ph);
             }
@@ -461,7 +464,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             for (int o = 0; o < SPLIT; ++o)
 #pragma unroll
                 for (int c = 0; c < OWN; ++c) sum[c] += o == member ? own[c] : from[(o * OWN + c) * 32];
-            P::template store<CG, BN>(p, t, sum, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS + member * OWN);
+            P::template store<CG, BN>(p, t, sum, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS + member * OWN, staging);
         }
     }
 
