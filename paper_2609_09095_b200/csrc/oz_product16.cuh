@@ -339,6 +339,8 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             }
         } else if (P::RAGGED_K && warp == 2) {
             // -------------------------------------------------------- inner indices behind the group's end
+            // One warp, all tiles in order: each wait is for the next phase of its barrier.  (Of two warps in turns one would wait for the phase after it
+            // where two tiles end in the same stage, and a wait on a parity returns at once while the phase before is open.)
             uint32_t tail_phase = 0;                         // bit s: phase of stage s's tail barrier
             const int64_t total = P::template total<CG, BN>(p, table, 0);
             for (int64_t item = first_item; ok && item < total; item += item_step) {
