@@ -329,6 +329,7 @@ oz_status_t oz_query_fallback_rows(void *stream, int64_t *rows);
  * aligned to their element type, nothing enqueued after a host-detectable error, internal work on `stream`
  * only), with these differences: no workspace registered with oz_set_workspace() is used, Inf and NaN go
  * through the arithmetic like in any FP32 product and set no status, and the exponent-span check does not apply.
+ * A device's first call of the library sets up its tables: make it outside a stream capture.
  * A row-major matrix is the column-major transpose: a (tokens, features) array of a framework is
  * a features x tokens matrix here, one column a token. */
 typedef enum { OZ_BF16 = 0, OZ_F16 = 1, OZ_F32 = 2 } oz_type_t;

@@ -105,6 +105,23 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8])
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// A wait for something that may be many tiles away: it ends with the others' waits, which are for the next block or tile, or after thirty times their limit.
+__device__ __forceinline__ bool mbar_wait_rare(uint32_t bar, uint32_t parity, volatile int *abort_flag, unsigned int *status)
+{
+    const unsigned long long start = global_timer_ns();
+    for (;;) {
+#pragma unroll 1
+        for (int it = 0; it < 256; ++it)
+            if (mbar_try_wait(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (global_timer_ns() - start > 30 * kWaitLimitNs) {
+            *abort_flag = 1;
+            atomicOr(status, 1u << OZ_ERR_TIMEOUT);
+            return false;
+        }
+    }
+}
+
 // arrivals at a barrier of any CTA of the cluster, ordered after this thread's (and, through it, its warp's) writes
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr)
 {
@@ -350,7 +367,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
                 const int last = (stage + mine - 1) % STAGES;
                 stage = (stage + mine) % STAGES;
                 if (!needs_tail(t) || mine == 0 || end_block(blocks) != blocks) continue;
-                ok = wait(tail_bar + 8 * last, (tail_phase >> last) & 1u);
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait_rare(tail_bar + 8 * last, (tail_phase >> last) & 1u, abort_flag, status)) != 0;
                 if (!ok) break;
                 tail_phase ^= 1u << last;
                 const int from = t.k_len & 63, to = (from + 15) & ~15;
