@@ -292,3 +292,52 @@ def test_one_matrix_for_all():
     for i in range(3):
         assert (got[i].double() - want[0].double()).norm() <= 2 * 140 ** 0.5 * spread_bound(5, USUAL, 1.3)
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
+
+
+@pytest.mark.parametrize("rows,cols", [(60, 90), (310, 300), (1, 5000), (2047, 128), (130, 5001)])
+def test_many_steps_reach_orthogonal_rows(rows, cols):
+    """The cubic iteration p(s) = (3 s - s^3) / 2 has p(1) = 1 and p'(1) = 0: what is left is one step's perturbation, 2^-20 max(1, |a| + |b|) = 2^-19 of the
+    2-norm, twice in O O^T and sqrt(r) of it in the Frobenius norm."""
+    o = update(tensor(1, rows, cols, seed=16), steps=40, coefficients=(1.5, -0.5, 0.0))[0].double()
+    o = o if rows <= cols else o.T
+    r = o.shape[0]
+    assert (o @ o.T - torch.eye(r, device="cuda", dtype=torch.float64)).norm() <= 2 * r ** 0.5 * 2.0 ** -19
+
+
+def test_beside_other_calls_of_the_library():
+    """Between emulated products on one stream, and three kinds of calls on three streams at once: the results of the same calls alone, bit for bit."""
+    a, b = tensor(1, 600, 700, seed=17), tensor(1, 100, 400, seed=18, dtype=torch.bfloat16)
+    want_a, want_b = update(a), update(b, torch.bfloat16)
+    x, w = tensor(900, 512, seed=19, dtype=torch.bfloat16), tensor(4, 640, 512, seed=20, dtype=torch.bfloat16, scale=0.05)
+    offsets = torch.tensor([0, 100, 600, 600, 900]).cuda()
+
+    def experts(y, stream=None):
+        oz.check(oz.oz_gemm_grouped(1, 640, 900, 512, 4, offsets, oz.OZ_BF16, w, 512, 640 * 512, x, 512, oz.OZ_BF16, 0.0, y, 640, stream))
+        return y
+
+    want_y = experts(torch.zeros(900, 640, dtype=torch.bfloat16, device="cuda"))
+    n = 512
+    A, B = (torch.randn(n, n, dtype=torch.float64, device="cuda") for _ in range(2))
+    C = torch.zeros(n, n, dtype=torch.float64, device="cuda")
+    product_space = torch.empty(oz.oz_workspace_bytes(n, n, n, oz.OZ_SET_S, 0), dtype=torch.uint8, device="cuda")
+    oz.check(oz.oz_set_workspace(product_space))
+    oz.check(oz.oz_dgemm(n, n, n, A, n, B, n, C, n))
+    want_c = C.clone()
+    spaces = [torch.empty(oz.oz_orthogonalise_workspace_bytes(g.shape[2], g.shape[1], 1), dtype=torch.uint8, device="cuda") for g in (a, b)]
+    out_a, out_b, out_y = torch.zeros_like(want_a), torch.zeros_like(want_b), torch.zeros_like(want_y)
+    for _ in range(5):
+        for call in (lambda: experts(out_y), lambda: update(a, out=out_a, workspace=spaces[0]), lambda: update(b, out=out_b, workspace=spaces[1])):
+            C.zero_()
+            oz.check(oz.oz_dgemm(n, n, n, A, n, B, n, C, n))
+            call()
+            assert torch.equal(C, want_c)
+    assert torch.equal(out_a, want_a) and torch.equal(out_b, want_b) and torch.equal(out_y, want_y)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        update(a, out=out_a, workspace=spaces[0], stream=streams[0])
+        update(b, out=out_b, workspace=spaces[1], stream=streams[1])
+        experts(out_y, streams[2])
+    torch.cuda.synchronize()
+    assert torch.equal(out_a, want_a) and torch.equal(out_b, want_b) and torch.equal(out_y, want_y)
+    oz.oz_set_workspace(None)
