@@ -284,6 +284,7 @@ struct GroupedPolicy {
     };
     using Maps = GroupedMaps;
     static constexpr bool RAGGED_K = INNER, COOPERATIVE = false;
+    static constexpr unsigned long long WAIT_NS = kWaitLimitNs;
     static constexpr int STAGING = ROWS ? P16_EPI_WARPS * 32 * 128 : 0;
     static __device__ __forceinline__ const CUtensorMap *map_a(const Maps &m, int) { return &m.a; }
     static __device__ __forceinline__ const CUtensorMap *map_b(const Maps &m, int) { return &m.b; }

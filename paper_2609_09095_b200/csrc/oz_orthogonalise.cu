@@ -36,7 +36,10 @@ constexpr int kMaxSteps = 100;
 constexpr int NORM_THREADS = 256;
 constexpr int MAX_PARTS = 192;                     // partial sums of squares of a matrix
 constexpr int PLANE_TILE = 64;
-constexpr unsigned long long kPhaseLimitNs = 4000000000ull;        // 4 s for the other blocks: twice what each of them waits for a barrier
+// Every wait of the launch of all steps, those of a block's warps for the next phase among them (a block without a tile waits with all of its
+// warps while the others multiply).  The longest phase: X X^T of one row, on one pair, of as many elements as fill the memory (512 bytes of planes
+// each), 350 million in 2.6 s.
+constexpr unsigned long long kPhaseLimitNs = 20000000000ull;
 
 template <class T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -313,6 +316,7 @@ struct NewtonPolicy {
         int matrix, phase;
     };
     static constexpr bool RAGGED_K = false, COOPERATIVE = true;
+    static constexpr unsigned long long WAIT_NS = kPhaseLimitNs;
     static constexpr int STAGING = 0;
 
     static __device__ __forceinline__ const CUtensorMap *map_a(const Maps &m, int phase)

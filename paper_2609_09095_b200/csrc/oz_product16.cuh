@@ -172,6 +172,7 @@ __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap
 //   P::a_mn(p, tile, block), P::b_mn(p, tile, block): whether the operand of the tile's block is stored along its rows (MN-major)
 //   P::STAGING             bytes of shared memory, off the ring, through which store() takes its results: a sixteenth an epilogue warp
 //   P::COOPERATIVE         the launch's blocks wait for one another (between phases)
+//   P::WAIT_NS             limit of a wait: longer than a tile's next step takes and, between phases, than the other blocks' tiles
 //   P::store<CG, BN>(p, tile, acc, row, col, staging): the thread's results, row of the tile (0 .. 128 CG - 1), as many columns from col on as acc
 //                          holds; called by whole warps
 template <class P, int CG, int BN, int PLANES, int SPLIT>
@@ -227,7 +228,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
     if (!P::COOPERATIVE) dependency_release();
     const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_base_ptr, 0);
     unsigned int *const status = p.core.status;
-    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status)) != 0; };
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag, status, P::WAIT_NS)) != 0; };
     // the member's blocks of a tile
     auto first_block = [&](int blocks) { return SPLIT == 1 ? 0 : static_cast<int>(static_cast<int64_t>(blocks) * member / SPLIT); };
     auto end_block = [&](int blocks) { return SPLIT == 1 ? blocks : static_cast<int>(static_cast<int64_t>(blocks) * (member + 1) / SPLIT); };

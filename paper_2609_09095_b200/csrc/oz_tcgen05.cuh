@@ -98,7 +98,7 @@ constexpr unsigned long long kWaitLimitNs = 2000000000ull;   // 2 s per wait
 // Bounded wait.  Returns false when the wait ran out or another role already gave up.
 // The timer is read only after a long run of failed polls: the common path never touches it.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag,
-                                          unsigned int *status)
+                                          unsigned int *status, unsigned long long limit_ns = kWaitLimitNs)
 {
 #pragma unroll 1
     for (int it = 0; it < 4096; ++it)
@@ -109,7 +109,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
         for (int it = 0; it < 256; ++it)
             if (mbar_try_wait(bar, parity)) return true;
         if (*abort_flag) return false;
-        if (global_timer_ns() - start > kWaitLimitNs) {
+        if (global_timer_ns() - start > limit_ns) {
             *abort_flag = 1;
             atomicOr(status, 1u << OZ_ERR_TIMEOUT);
             return false;

@@ -341,3 +341,23 @@ def test_beside_other_calls_of_the_library():
     torch.cuda.synchronize()
     assert torch.equal(out_a, want_a) and torch.equal(out_b, want_b) and torch.equal(out_y, want_y)
     oz.oz_set_workspace(None)
+
+
+def test_phases_of_seconds():
+    """X X^T of one row is one tile: the other blocks wait for it through 350 million elements, more than 2 s.  4096 of them are +-1 and all others zero,
+    so that X = G / 64, X X^T = 1 and 2 X - 1.5 X + 0.5 X = X are exact."""
+    n = 350_000_000
+    torch.cuda.empty_cache()
+    need = oz.oz_orthogonalise_workspace_bytes(n, 1, 1)
+    if torch.cuda.mem_get_info()[0] < need + 6 * n + (3 << 30):
+        pytest.skip("the planes of this row fill a whole device")
+    try:
+        g = torch.zeros(1, 1, n, dtype=torch.bfloat16, device="cuda")
+        at = torch.arange(4096, device="cuda") * 85_000 + 17
+        g[0, 0, at] = (1.0 - 2.0 * (at % 2)).bfloat16()
+        got = update(g, steps=1, coefficients=(2.0, -1.5, 0.5), eps=0.0, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"))
+        assert oz.oz_query_status() in (oz.OZ_OK, oz.OZ_ERR_RANGE)
+        assert torch.equal(got[0, 0, at], g[0, 0, at].float() / 64) and torch.count_nonzero(got).item() == 4096
+    finally:
+        g = got = None
+        torch.cuda.empty_cache()
