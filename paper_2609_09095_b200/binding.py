@@ -116,11 +116,14 @@ _torch = None
 
 def _stream(stream) -> int:
     if stream is None:
-        # the handle itself: building a stream object for it takes longer than a launch
+        # the handle itself, where torch gives it: building a stream object for it takes longer than a launch
         global _torch
         if _torch is None:
             import torch as _torch
-        return _torch._C._cuda_getCurrentRawStream(_torch.cuda.current_device())
+        handle = getattr(_torch._C, "_cuda_getCurrentRawStream", None)
+        if handle is None:
+            return _torch.cuda.current_stream().cuda_stream
+        return handle(_torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
