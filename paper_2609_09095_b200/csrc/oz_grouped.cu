@@ -6,9 +6,6 @@
 //
 // The groups' offsets are on the device, written by whatever sorts the tokens, so that the tiles of a launch are counted on the
 // device too: every block reads the offsets, counts the tiles of each group and walks the list of all tiles.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <atomic>
 #include <type_traits>
 #include <utility>
@@ -93,16 +90,6 @@ __device__ __forceinline__ int group_of(const int *before, int groups, int t)
     }
     return lo;
 }
-
-template <class T> __device__ __forceinline__ float to_float(T v);
-template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-
-template <class T> __device__ __forceinline__ T from_float(float v);
-template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
-template <> __device__ __forceinline__ float from_float(float v) { return v; }
-template <> __device__ __forceinline__ float to_float(float v) { return v; }
 
 // c[i ldc] = acc[i] of the first `valid` columns, or the sum with what is there, rounded once either way; old values a few at a time
 template <class T, bool ACCUMULATE, int N>

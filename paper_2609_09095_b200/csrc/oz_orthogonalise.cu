@@ -19,9 +19,6 @@
 // three times that on the pipe.  Five steps: 4096 x 4096 in FP32 3.7 ms, 1.1 PFLOP/s on the pipe (power cap; the FP32 iteration of a library 34);
 // 16 x 512 x 2048 603 us (gram on 48 of 74 pairs, 256 tiles of P X in 4 rounds); 1024 x 1024 168 us, 10 us a phase: 6.6 of them products, the rest
 // storing, meeting and the first copies.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -40,15 +37,6 @@ constexpr int PLANE_TILE = 64;
 // warps while the others multiply).  The longest phase: X X^T of one row, on one pair, of as many elements as fill the memory (512 bytes of planes
 // each), 350 million in 2.6 s.
 constexpr unsigned long long kPhaseLimitNs = 20000000000ull;
-
-template <class T> __device__ __forceinline__ float to_float(T v);
-template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float to_float(float v) { return v; }
-template <class T> __device__ __forceinline__ T from_float(float v);
-template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
-template <> __device__ __forceinline__ float from_float(float v) { return v; }
 
 __device__ __forceinline__ void store_number(void *X, int64_t at, float v, int type)
 {

@@ -18,11 +18,11 @@
 // A persistent CTA of 19 warps per multiprocessor:
 //   warp 0       bulk copies into a ring of shared memory (no multicast)
 //   warp 1       issues the MMAs (of a pair: the leader's)
-//   warp 2       RAGGED_K: zeroes, in the last block of a tile, the inner indices that belong to the next group, in both operands
-//                (zeroing one would leave 0 x NaN)
+//   warp 2       RAGGED_K (pairs only): zeroes, in the last block of a tile, the inner indices that belong to the next group, in both
+//                operands (zeroing one would leave 0 x NaN)
 //   warps 3..18  epilogue, four per lane quarter of the tensor memory, BN / 4 columns each
 //
-// SPLIT > 1: products of so few tiles that most multiprocessors would have none.  A cluster of SPLIT pairs (or single CTAs) shares one tile, each
+// SPLIT > 1: products of so few tiles that most multiprocessors would have none.  A cluster of SPLIT single CTAs shares one tile, each
 // member a range of the inner dimension; at the end every member owns BN / SPLIT columns, gets the others' sums of them through shared
 // memory of the cluster (in the ring, which nothing fills any more), adds them in the order of the members and stores.  One tile a cluster.
 //
@@ -32,9 +32,21 @@
 // holds none of what the predecessor still has to take.  (Cooperative launches neither wait nor let in.)
 #pragma once
 
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
 #include "oz_tcgen05.cuh"
 
 namespace oz {
+
+template <class T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_float(float v) { return v; }
+template <class T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ float from_float(float v) { return v; }
 
 constexpr int P16_THREADS = 19 * 32;
 constexpr int P16_FIRST_EPI = 3;
@@ -134,24 +146,12 @@ __device__ __forceinline__ void mbar_expect_tx_cluster(uint32_t cluster_addr, ui
     asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(cluster_addr), "r"(bytes) : "memory");
 }
 
-// mbarrier arrives in both CTAs of the pair that begins at cluster rank `pair` once every MMA issued so far by this thread has completed
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint32_t pair)
-{
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"(static_cast<uint16_t>(3u << pair)) : "memory");
-}
-
 __device__ __forceinline__ void store_cluster(uint32_t cluster_addr, float v)
 {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(cluster_addr), "f"(v) : "memory");
 }
 
 // 64 elements x 64 lines of a plane of a matrix in plane pairs: (element, chunk and plane, line, matrix)
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2, int c3)
-{
-    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
-                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
-}
 __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap *map, uint32_t bar_cluster, int c0, int c1, int c2, int c3)
 {
     asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -181,10 +181,11 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
 {
     using R = Ring16<CG, BN, PLANES, P::STAGING>;
     constexpr int STAGES = R::STAGES;
-    constexpr int TMEM_COLUMNS = 2 * BN < 32 ? 32 : 2 * BN;
+    constexpr int TMEM_COLUMNS = 2 * BN;
+    static_assert(CG == 2 ? SPLIT == 1 : (PLANES == 1 && !P::RAGGED_K), "single CTAs share tiles; pairs have plane pairs and ragged ends");
     const uint32_t place = CG * SPLIT > 1 ? cluster_ctarank() : 0u;
-    const uint32_t rank = place % CG, pair = place - rank;          // in the pair, and the pair's first CTA
-    const int member = static_cast<int>(place / CG);                // of the SPLIT that share a tile
+    const uint32_t rank = CG == 2 ? place : 0u;                     // in the pair, whose first CTA leads
+    const int member = CG == 2 ? 0 : static_cast<int>(place);       // of the SPLIT that share a tile
     const int64_t first_item = blockIdx.x / (CG * SPLIT);
     const int64_t item_step = gridDim.x / (CG * SPLIT);
     extern __shared__ unsigned char smem_raw[];
@@ -266,18 +267,17 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
                     if (leader) {
                         uint32_t bar;
                         if (CG == 1) {
-                            bar = (tail ? tail_bar : full_bar) + 8 * stage;
+                            bar = full_bar + 8 * stage;
                             mbar_expect_tx(bar, bytes);
                         } else {
-                            bar = tail ? map_to_cta(tail_bar + 8 * stage, place) : map_to_cta(full_bar + 8 * stage, pair);
+                            bar = tail ? map_to_cta(tail_bar + 8 * stage, rank) : map_to_cta(full_bar + 8 * stage, 0u);
                             mbar_expect_tx_cluster(bar, bytes);
                         }
                         const int a_mn = P::a_mn(p, t, kb), b_mn = P::b_mn(p, t, kb);
                         auto copy = [&](uint32_t dst, const CUtensorMap *map, int mn, int row, int z, int plane) {
                             const int c0 = mn ? row : kk, c1 = mn ? kk : row;
                             if constexpr (PLANES == 2) {
-                                if (CG == 1) tma_load_4d(dst, map, bar, c0 & 63, 2 * (c0 >> 6) + plane, c1, z);
-                                else tma_load_4d_pair(dst, map, bar, c0 & 63, 2 * (c0 >> 6) + plane, c1, z);
+                                tma_load_4d_pair(dst, map, bar, c0 & 63, 2 * (c0 >> 6) + plane, c1, z);
                             } else {
                                 if (CG == 1) tma_load_3d(dst, map, bar, c0, c1, z);
                                 else tma_load_3d_pair(dst, map, bar, c0, c1, z);
@@ -340,16 +340,12 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
                                 for (int ks = 0; ks < 4; ++ks)
                                     if (ks * 16 < left) umma16<CG>(d, a + ks * step_a, b + ks * step_b, idesc, kb > kb0 || ks > 0 ? 1u : 0u);
                             }
-                            if constexpr (CG == 2) umma_commit_pair(empty_bar + 8 * stage, pair);
-                            else umma_commit<1>(empty_bar + 8 * stage);
+                            umma_commit<CG>(empty_bar + 8 * stage);
                         }
                         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
                     }
                     if (!ok) break;
-                    if (leader) {
-                        if constexpr (CG == 2) umma_commit_pair(tfull_bar + 8 * slot, pair);
-                        else umma_commit<1>(tfull_bar + 8 * slot);
-                    }
+                    if (leader) umma_commit<CG>(tfull_bar + 8 * slot);
                     slot_phase ^= 1u << slot;
                     slot ^= 1;
                 }
@@ -364,10 +360,9 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             for (int64_t item = first_item; ok && item < total; item += item_step) {
                 const typename P::Tile t = P::template decode<CG, BN>(p, table, 0, item);
                 const int blocks = (t.k_len + P16_BLOCK_K - 1) / P16_BLOCK_K;
-                const int mine = end_block(blocks) - first_block(blocks);
-                const int last = (stage + mine - 1) % STAGES;
-                stage = (stage + mine) % STAGES;
-                if (!needs_tail(t) || mine == 0 || end_block(blocks) != blocks) continue;
+                const int last = (stage + blocks - 1) % STAGES;
+                stage = (stage + blocks) % STAGES;
+                if (!needs_tail(t)) continue;
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait_rare(tail_bar + 8 * last, (tail_phase >> last) & 1u, abort_flag, status)) != 0;
                 if (!ok) break;
                 tail_phase ^= 1u << last;
@@ -382,10 +377,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
                         if (from + lane / 8 + row < to) *reinterpret_cast<uint4 *>(first + box * P16_BOX_BYTES + row * 128) = make_uint4(0u, 0u, 0u, 0u);
                 asm volatile("fence.proxy.async;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    if (CG == 1) mbar_arrive(full_bar + 8 * last);
-                    else mbar_arrive_cluster(map_to_cta(full_bar + 8 * last, pair));
-                }
+                if (lane == 0) mbar_arrive_cluster(map_to_cta(full_bar + 8 * last, 0u));
             }
         }
         if (!ok) {
@@ -424,7 +416,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             __syncwarp();
             if (lane == 0) {
                 if (CG == 1) mbar_arrive_relaxed(tempty_bar + 8 * slot);
-                else mbar_arrive_cluster_relaxed(map_to_cta(tempty_bar + 8 * slot, pair));
+                else mbar_arrive_cluster_relaxed(map_to_cta(tempty_bar + 8 * slot, 0u));
             }
             slot_phase ^= 1u << slot;
             slot ^= 1;
@@ -463,7 +455,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
 #pragma unroll
             for (int o = 0; o < SPLIT; ++o)
                 if (o != member) {
-                    const uint32_t to = map_to_cta(box + static_cast<uint32_t>(member * OWN * 128), static_cast<uint32_t>(o * CG) + rank);
+                    const uint32_t to = map_to_cta(box + static_cast<uint32_t>(member * OWN * 128), static_cast<uint32_t>(o));
 #pragma unroll
                     for (int c = 0; c < OWN; ++c) store_cluster(to + c * 128, acc[o * OWN + c]);
                 }
@@ -484,7 +476,7 @@ product16_kernel(const __grid_constant__ typename P::Maps maps, const __grid_con
             for (int o = 0; o < SPLIT; ++o)
 #pragma unroll
                 for (int c = 0; c < OWN; ++c) sum[c] += o == member ? own[c] : from[(o * OWN + c) * 32];
-            P::template store<CG, BN>(p, t, sum, static_cast<int>(rank) * 128 + q * 32 + lane, part * R::COLS + member * OWN, staging);
+            P::template store<CG, BN>(p, t, sum, q * 32 + lane, part * R::COLS + member * OWN, staging);
         }
     }
 
