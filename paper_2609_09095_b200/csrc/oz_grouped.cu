@@ -424,10 +424,13 @@ oz_status_t launch_tensor(GroupedParams p, oz_type_t type, bool *taken, cudaStre
     const bool bf16 = type == OZ_BF16;
     p.a_mn = p.rowA == 1 && p.innerA != 1;
     p.core.status = p.status;
-    // Segments of 512 inner indices for FP32 results: error against 64 bits of the weight gradients of 16 experts, 16384 tokens, 4.4e-7, and 302 us; with
-    // segments of 256 2.3e-7 and 332 us (the epilogue, still storing the tile before, holds up the MMAs after two segments).  Of 4096 for 16-bit
-    // results, which keeps what is cut off, 2^-24 of the sum 256 times in the mean, a tenth of a half-precision rounding.
-    p.core.seg = p.ctype == OZ_F32 ? 8 : 64;
+    // Segments of 320 inner indices for FP32 results, about the error of a product that rounds every FP32 addition.  Error against 64 bits and us with
+    // 256 / 320 / 384 / 512, weight gradients 2048 x 4096 of 16 experts, 16384 tokens (such a product: 2.8e-7): 2.3e-7, 273 / 2.8e-7, 268 / 3.3e-7, 265 /
+    // 4.4e-7, 265; input gradients of the same (3.9e-7): 2.4e-7, 237 / 2.9e-7, 230 / 3.4e-7, 229 / 4.7e-7, 225; forward, 8192 tokens, 8 experts 4096 x
+    // 4096 (6.1e-7): 2.4e-7, 229 / 2.9e-7, 217 / 3.5e-7, 214 / 4.8e-7, 214.  (The epilogue adds up every segment, and, still storing the tile before,
+    // holds up the MMAs after two.)  Of 4096 for 16-bit results, which keeps what is cut off, 2^-24 of the sum 256 times in the mean, a tenth of a
+    // half-precision rounding.
+    p.core.seg = p.ctype == OZ_F32 ? 5 : 64;
     const TileShape shape = INNER ? TileShape{2, 256, 1} : tile_shape(p);
     GroupedMaps maps;
     const int64_t za = p.shared_a ? 1 : p.groups;

@@ -328,3 +328,18 @@ def test_broadcast_inputs():
     for g, count in ((0, 100), (1, 30)):
         exact = count * x[0].double()
         assert ((grad[g].double() - exact).abs() <= (count + 1) * 2.0 ** -23 * exact.abs()).all()
+
+
+def test_fp32_results_lose_as_little_as_fp32_sums():
+    """Sums of positive numbers, of which the tensor core only ever cuts off.  An accumulator takes 320 inner indices in 20 additions and grows evenly;
+    each addition loses half a unit in the mean, at most 2^-24 of what the accumulator then holds, together (20 + 1) / 2 2^-24 of a segment.  What is
+    rounded to nearest afterwards has no mean."""
+    K = 4096
+    x, w = tensor(64, K, dtype=torch.bfloat16, seed=37).abs(), tensor(1, 320, K, dtype=torch.bfloat16, seed=38).abs()
+    y = run_grouped(x, w, offsets_of([64]), torch.zeros(64, 320, device="cuda"), 1)
+    dx = run_grouped(x, w.transpose(1, 2).contiguous(), offsets_of([64]), torch.zeros(64, 320, device="cuda"), 0)
+    grad = run_wgrad(w[0].T.contiguous(), x.T.contiguous(), offsets_of([K]), torch.zeros(1, 64, 320, device="cuda"))[0]
+    exact = x.double() @ w[0].double().T
+    for got in (y, dx, grad):
+        loss = ((exact - got.double()) / exact).mean().item()
+        assert abs(loss) <= 10.5 * 2.0 ** -24, loss * 2 ** 24
