@@ -524,14 +524,15 @@ oz_status_t launch_newton(const NewtonMaps &maps, const NewtonParams &p, cudaStr
     return launch_product16<NewtonPolicy<FOLDED>, 2, BN, 2, 1>(maps, p, most, 0, stream);
 }
 
-// cycles of a step with tiles of 256 x BN: rounds over the pairs, blocks of 64 inner indices at `each` cycles
+// cycles of a step with tiles of 256 x BN: rounds over the pairs, each with its blocks of 64 inner indices and `store` cycles for what a round
+// takes besides
 template <int BN>
-int64_t step_cycles(const NewtonParams &p, int each)
+int64_t step_cycles(const NewtonParams &p, int block, int store)
 {
     int64_t sum = 0;
     for (int phase = 0; phase < 3; ++phase) {
         const int64_t tiles = static_cast<int64_t>(p.count) * newton_tiles<BN>(p.r, p.c, phase), pairs = sm_count() / 2;
-        sum += (tiles + pairs - 1) / pairs * (((phase == kGram ? p.c : p.r) + 63) / 64 * each);
+        sum += (tiles + pairs - 1) / pairs * (((phase == kGram ? p.c : p.r) + 63) / 64 * block + store);
     }
     return sum;
 }
@@ -1102,9 +1103,16 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     std::copy(alpha, alpha + 3 * steps, p.alpha);
     std::copy(beta, beta + 3 * steps, p.beta);
     std::copy(diagonal, diagonal + steps, p.diagonal);
-    // Cycles of a block of 64 inner indices: the tensor cores' 1536 with 256 columns, shared memory's with fewer.  Columns 256 / 128 / 64 in us: 1024 x 1024
-    // 375 / 247 / 256, 3 x 1009 x 517 326 / 302 / 281, 16 x 512 x 2048 764 / 720 / 841, 4096 x 4096 3593 / 3519 / 5062 (all before blocks asked once).
-    const int64_t wide = step_cycles<256>(p, 1536), half = step_cycles<128>(p, 960), narrow = step_cycles<64>(p, 790);
+    // Cycles of a block of 64 inner indices and of a round's store and meeting, fitted to five steps of 53 sizes (at the power cap those that reach it); FP32
+    // results, whose accumulators are read after every block, apart from 16-bit ones.  The pick is within 4 percent of the fastest width for all of them,
+    // 0.1 in the mean (by the products' cycles alone 12 and 1.3).  us with 256 / 128 / 64 columns, the pick marked:
+    //   FP32      300 x 300  195 / 126 / 118*       1024 x 1024  349 / 230 / 209*      3 x 1009 x 517  297 / 199* / 211   12 x 520 x 520  344 / 326* / 443
+    //             2048 x 2048  639 / 569* / 856     16 x 512 x 2048  750* / 758 / 944  3000 x 3000  1820 / 1790* / 2681   4096 x 4096  3729* / 3890 / 6623
+    //   bfloat16  300 x 300  172 / 117 / 103*       1024 x 1024  331 / 205 / 168*      3 x 1009 x 517  278 / 185 / 173*   12 x 520 x 520  298 / 265* / 329
+    //             2048 x 2048  582 / 502* / 630     16 x 512 x 2048  603* / 619 / 731  3000 x 3000  1626 / 1546* / 1980   4096 x 4096  3302* / 3354 / 4853
+    const int64_t wide = folded ? step_cycles<256>(p, 1600, 12000) : step_cycles<256>(p, 1600, 13600),
+                  half = folded ? step_cycles<128>(p, 995, 5170) : step_cycles<128>(p, 994, 5900),
+                  narrow = folded ? step_cycles<64>(p, 571, 5690) : step_cycles<64>(p, 1036, 2500);
     if (wide <= half && wide <= narrow) return folded ? launch_newton<true, 256>(maps, p, s) : launch_newton<false, 256>(maps, p, s);
     if (half <= narrow) return folded ? launch_newton<true, 128>(maps, p, s) : launch_newton<false, 128>(maps, p, s);
     return folded ? launch_newton<true, 64>(maps, p, s) : launch_newton<false, 64>(maps, p, s);
