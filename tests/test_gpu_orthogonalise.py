@@ -361,3 +361,95 @@ def test_phases_of_seconds():
     finally:
         g = got = None
         torch.cuda.empty_cache()
+
+
+def poisoned_workspace(cols, rows, count):
+    """All bits set: every half-precision number in it is NaN, and what is read before it is written shows."""
+    return torch.full((oz.oz_orthogonalise_workspace_bytes(cols, rows, count),), 0xFF, dtype=torch.uint8, device="cuda")
+
+
+# tiles of 64, 128 and 256 columns, one to six blocks of 256 rows, X as it is and transposed, borders inside a tile
+@pytest.mark.parametrize("count,rows,cols", [(1, 310, 300), (2, 300, 310), (1, 257, 1030), (1, 1400, 1450), (12, 520, 520), (2, 1501, 1300), (16, 512, 2048), (16, 2047, 510)])
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.float32, torch.float16), (torch.float16, torch.bfloat16)])
+def test_general_form_element_by_element(count, rows, cols, dtype, out_dtype):
+    """One step, all matrices.  16-bit results take a X in through P's diagonal: P + a I is held in planes, whose bound has a beside b and c, and its product
+    with X loses kappa of a |X| more."""
+    a = USUAL[0]
+    g = tensor(count, rows, cols, seed=21, dtype=dtype)
+    got = update(g, out_dtype, 1, workspace=poisoned_workspace(cols, rows, count))
+    assert oz.oz_query_status() in (oz.OZ_OK, oz.OZ_ERR_RANGE)
+    for i in range(count):
+        x, y = normalised(g[i], 1e-7), got[i].double()
+        x, y = (x, y) if rows <= cols else (x.T, y.T)
+        exact, e = iterate(x, 1, USUAL), step_bound(x, USUAL)
+        if out_dtype != torch.float32:
+            ax = x.abs()
+            e = e + 1.02 * a * ((RHO + kappa(x.shape[0]) + 4 * U24) * ax + 2.0 ** -38 * ax.sum(0))
+        tol = e + (exact.abs() + e) * torch.finfo(out_dtype).eps / 2 + (2.0 ** -25 if out_dtype == torch.float16 else 0.0)
+        off = (y - exact).abs()
+        assert (off <= tol).all(), (i, float((off / tol).nan_to_num(float("inf")).max()))
+
+
+def fp32_error(x, steps=5):
+    """The exact update of X and how far the usual iteration in FP32 is off, in the Frobenius norm."""
+    exact = iterate(x, steps, USUAL)
+    return exact, (iterate(x.float(), steps, USUAL).double() - exact).norm()
+
+
+def hold_near(got, g, eps=1e-7):
+    """Every matrix no further off than 4 errors of the FP32 iteration and the rounding of the result."""
+    for i in range(g.shape[0]):
+        exact, fp32 = fp32_error(normalised(g[i], eps))
+        off = (got[i].double() - exact).norm()
+        assert off <= 4 * fp32 + 2 * exact.norm() * torch.finfo(got.dtype).eps / 2, (i, float(off / exact.norm()))
+
+
+@pytest.mark.parametrize("count,rows,cols", [(3, 300, 260), (2, 260, 300), (4, 700, 150), (3, 90, 120), (2, 520, 530)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_strided_batch_close(count, rows, cols, dtype):
+    """All matrices of a strided batch against 64 bits, and element by element against the contiguous call: both are within 4 errors of the FP32
+    iteration of the exact update before they are rounded, each by half a step."""
+    g = tensor(count, rows, cols, seed=22, dtype=dtype)
+    want = update(g, dtype, workspace=poisoned_workspace(cols, rows, count))
+    hold_near(want, g)
+    source = torch.zeros(count, rows + 2, cols + 5, dtype=dtype, device="cuda")
+    source[:, 1:1 + rows, 3:3 + cols] = g
+    held = torch.full((count * (rows * (cols + 3) + 7) + 1,), 5.0, dtype=dtype, device="cuda")
+    out = held[1:].as_strided((count, rows, cols), (rows * (cols + 3) + 7, cols + 3, 1))
+    got = update(source[:, 1:1 + rows, 3:3 + cols], out=out, workspace=poisoned_workspace(cols, rows, count))
+    hold_near(got, g)
+    for i in range(count):
+        _, fp32 = fp32_error(normalised(g[i], 1e-7))
+        w = want[i].double().abs()
+        assert ((got[i].double() - want[i].double()).abs() <= 8 * fp32 + torch.finfo(dtype).eps * (w + 8 * fp32)).all(), i
+
+
+@pytest.mark.parametrize("rows,cols", [(40, 30), (300, 200)])
+def test_scales_close(rows, cols):
+    """From the largest numbers to subnormal ones: the update does not depend on the scale."""
+    for scale in (1e37, 1e-3, 1e-37, 1e-43):
+        g = tensor(2, rows, cols, seed=23) * scale
+        hold_near(update(g, eps=0.0, workspace=poisoned_workspace(cols, rows, 2)), g, eps=0.0)
+    assert oz.oz_query_status() in (oz.OZ_OK, oz.OZ_ERR_RANGE)
+
+
+@pytest.mark.parametrize("rows,cols", [(200, 140), (100, 90)])
+def test_one_matrix_for_all_close(rows, cols):
+    g = tensor(1, rows, cols, seed=24)
+    got = update(g[0].as_strided((3, rows, cols), (0, cols, 1)), workspace=poisoned_workspace(cols, rows, 3))
+    hold_near(got, g.expand(3, rows, cols))
+
+
+def test_update_of_experts_gradients_close():
+    """Gradients of uneven groups, an empty one among them, straight into the update."""
+    sizes, m, k = [300, 0, 41, 171], 136, 264
+    offsets = torch.tensor([0] + sizes).cumsum(0).cuda()
+    n, groups = sum(sizes), len(sizes)
+    x, dy = tensor(n, k, seed=25, dtype=torch.bfloat16), tensor(n, m, seed=26, dtype=torch.bfloat16)
+    for dw_dtype in (torch.float32, torch.bfloat16):
+        dw = torch.zeros(groups, m, k, dtype=dw_dtype, device="cuda")
+        oz.check(oz.oz_gemm_grouped_wgrad(k, m, n, groups, offsets, oz.OZ_BF16, x, k, dy, m, TYPE[dw_dtype], 0.0, dw, k, m * k))
+        o = update(dw, workspace=poisoned_workspace(k, m, groups))
+        assert not o[1].any()
+        used = [0, 2, 3]
+        hold_near(o[used], dw[used])
