@@ -343,3 +343,63 @@ def test_fp32_results_lose_as_little_as_fp32_sums():
     for got in (y, dx, grad):
         loss = ((exact - got.double()) / exact).mean().item()
         assert abs(loss) <= 10.5 * 2.0 ** -24, loss * 2 ** 24
+
+
+# 16-bit results of at most 256 tokens a group leave by rows, through shared memory, where C's columns begin on 16 bytes: widths that end inside eight
+# numbers, inside the 64 of a warp and inside a tile, with numbers behind them that stay
+@pytest.mark.parametrize("m,k", [(1, 1), (5, 7), (40, 33), (129, 100), (257, 259), (300, 516), (64, 1027)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_wgrad_by_rows_ends_anywhere(m, k, dtype):
+    sizes = [100, 0, 37, 1, 250]
+    offsets = offsets_of(sizes, 3)
+    n, groups = 3 + sum(sizes) + 2, len(sizes)
+
+    def padded(cols, seed, scale):
+        ld = (cols + 7) // 8 * 8
+        return tensor(n, ld, dtype=dtype, seed=seed, scale=scale)[:, :cols]
+
+    x, dy = padded(k, 39, 1.0), padded(m, 40, 0.1)
+    ldc = (k + 7) // 8 * 8 + 8
+    stride = m * ldc + 16
+    held = torch.full((groups * stride,), 9.0, dtype=dtype, device="cuda")
+    grad = held.as_strided((groups, m, k), (stride, ldc, 1))
+    run_wgrad(x, dy, offsets, grad)
+    cuts = offsets.tolist()
+    for g, (lo, hi) in enumerate(zip(cuts, cuts[1:])):
+        a, b = dy[lo:hi].double(), x[lo:hi].double()
+        within(grad[g], a.T @ b, a.abs().T @ b.abs(), hi - lo, f"group {g}")
+    mask = torch.ones_like(held, dtype=torch.bool)
+    mask.as_strided((groups, m, k), (stride, ldc, 1))[:] = False
+    assert (held[mask] == 9.0).all(), "behind the rows"
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_16_bit_results_of_long_sums(dtype):
+    """Sums of positive numbers over more than two accumulators of 4096 inner indices.  Each of the 256 additions to an accumulator, and the sixteen's own
+    sum, cuts off less than 2^-23 of what the accumulator holds at its end, the additions of the accumulators round by 2^-24; then one rounding
+    to the type."""
+    K = 9000
+    x, w = tensor(5, K, dtype=dtype, seed=41).abs(), tensor(1, 136, K, dtype=dtype, seed=42, scale=1 / 64).abs()
+    y = run_grouped(x, w, offsets_of([5]), torch.zeros(5, 136, dtype=dtype, device="cuda"), 1)
+    xs, ws = torch.zeros(K, 8, dtype=dtype, device="cuda"), w[0].T.contiguous()
+    xs[:, :5] = x.T
+    grad = run_wgrad(ws, xs, offsets_of([K]), torch.zeros(1, 8, 136, dtype=dtype, device="cuda"))[0, :5]
+    exact = x.double() @ w[0].double().T
+    lost = 257 * 2.0 ** -23 + 3 * 2.0 ** -24
+    for got in (y, grad):
+        assert ((got.double() - exact).abs() <= exact * (lost + (1 + lost) * torch.finfo(dtype).eps / 2)).all()
+
+
+def test_same_call_same_bits():
+    """All forms that a launch can take, three times each."""
+    for groups, each, m, k in ((1, 1, 2048, 1024), (8, 2, 512, 512), (16, 40, 1000, 520), (4, 700, 1304, 328), (2, 33, 41, 37)):
+        sizes = [each + (g % 3) * (each // 4) for g in range(groups)]
+        offsets = offsets_of(sizes)
+        n = sum(sizes)
+        x, w, dy = tensor(n, k, dtype=torch.bfloat16, seed=43), tensor(groups, m, k, dtype=torch.bfloat16, seed=44, scale=k ** -0.5), tensor(n, m, dtype=torch.bfloat16, seed=45)
+        for out in (torch.bfloat16, torch.float32):
+            y = [run_grouped(x, w, offsets, torch.zeros(n, m, dtype=out, device="cuda"), 1) for _ in range(3)]
+            dx = [run_grouped(dy, w, offsets, torch.zeros(n, k, dtype=out, device="cuda"), 0) for _ in range(3)]
+            dw = [run_wgrad(x, dy, offsets, torch.zeros(groups, m, k, dtype=out, device="cuda")) for _ in range(3)]
+            for r in (y, dx, dw):
+                assert torch.equal(r[0], r[1]) and torch.equal(r[0], r[2])
