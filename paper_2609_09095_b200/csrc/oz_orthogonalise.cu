@@ -4,10 +4,10 @@
 //
 // The products run on the 16-bit tensor pipe to the accuracy of FP32.  An iterate held in 16 bits would not do: what is lost in a step
 // is taken up by up to |a| (3.44 with the usual coefficients) in each of the next, and the update is off by 2e-3 beyond its own
-// rounding.  So a matrix is the sum of two half-precision planes hi + lo, 22 bits, of its elements times a power of two that
-// uses the range up to 2^15: hi is the rounded element, lo the rounded rest.  Of the four plane products lo lo lies below the last bit; the
-// other three go into one accumulator (PLANES = 2 of the product core).  Elements above 2^-18 of the bound keep all 22 bits, smaller ones an
-// absolute 2^-40 of it.
+// rounding.  So a matrix is the sum of two half-precision planes hi + lo, 22 bits, of its elements times the largest power of two that
+// keeps them, and 1 percent for roundings, within 2^15: hi is the rounded element, lo the rounded rest.  Of the four plane products lo lo lies below the
+// last bit; the other three go into one accumulator (PLANES = 2 of the product core).  The bound of the elements lies above 2^13.9 then: those above
+// 2^-17 of it keep all 22 bits, smaller ones an absolute 2^-39 of it (half of 2^-24, the step of the smallest half-precision numbers).
 //
 // Planes in memory: [matrix][line][chunk of 64 elements][hi, lo][64], so that both halves of an element lie at a fixed distance, and a block
 // of an operand is the same box whether its lines or its elements are the inner dimension.  Elements behind the last are zero.

@@ -80,7 +80,7 @@ struct Core16 {
 struct Tile16 {
     int a_row, a_z, b_row, b_z; // coordinates of the tile's first row of A and column of B
     int k_begin, k_len;
-    int cols;                   // columns computed: a multiple of 16 CG; of plane pairs, whose operand B may be along its rows, 64 or a multiple of 128
+    int cols;                   // columns computed: a multiple of 16, for pairs too; of plane pairs, whose operand B may be along its rows, 64 or a multiple of 128
 };
 
 __host__ __device__ inline uint32_t idesc16(bool bf16, int cg)
