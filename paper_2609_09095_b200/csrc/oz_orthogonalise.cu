@@ -16,8 +16,8 @@
 // both by the same bulk copies.  S and P are symmetric and computed on and below the diagonal only (see NewtonPolicy).
 //
 // Launches: sum of squares, planes of X, all products; narrow matrices: one.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
-// three times that on the pipe.  Five steps: 4096 x 4096 in FP32 3.7 ms, 1.1 PFLOP/s on the pipe (power cap; the FP32 iteration of a library 34);
-// 16 x 512 x 2048 603 us (gram on 48 of 74 pairs, 256 tiles of P X in 4 rounds); 1024 x 1024 168 us, 10 us a phase: 6.6 of them products, the rest
+// three times that on the pipe.  Five steps: 4096 x 4096 in FP32 3.6 ms, 1.15 PFLOP/s on the pipe (power cap; the FP32 iteration of a library 34);
+// 16 x 512 x 2048 in bfloat16 600 us (gram on 48 of 74 pairs, 256 tiles of P X in 4 rounds); 1024 x 1024 168 us, 10 us a phase: 6.6 of them products, the rest
 // storing, meeting and the first copies.
 #include <algorithm>
 #include <atomic>
@@ -407,7 +407,7 @@ struct NewtonPolicy {
         return t.phase % 3 == kGram || (t.phase % 3 == kPolynomial && block >> 2 < t.b_row >> 8);
     }
 
-    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and N columns, eight at a time.
+    // A thread has one row of X, S or P (consecutive lanes consecutive rows) and N columns, a few at a time.
     template <int CG, int BN, int N>
     static __device__ __forceinline__ void store(const Params &p, const Tile &t, const float (&acc)[N], int row, int col, unsigned char *)
     {
@@ -442,24 +442,24 @@ struct NewtonPolicy {
         }
     }
 
-    // v = alpha acc + beta old of columns c0 .. c0 + 7; `old` moves on.  (Written by other blocks of this launch: from L2.)
-    template <bool FULL, bool OLD, int N>
-    static __device__ __forceinline__ void results(float (&v)[8], const __half *&old, int64_t ld, const float (&acc)[N], int c0, float alpha,
+    // v = alpha acc + beta old of columns c0 .. c0 + K - 1; `old` moves on.  (Written by other blocks of this launch: from L2.)
+    template <bool FULL, bool OLD, int K, int N>
+    static __device__ __forceinline__ void results(float (&v)[K], const __half *&old, int64_t ld, const float (&acc)[N], int c0, float alpha,
                                                    float beta, int left)
     {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) v[c] = alpha * acc[c0 + c];
+        for (int c = 0; c < K; ++c) v[c] = alpha * acc[c0 + c];
         if constexpr (OLD) {
-            __half hi[8], lo[8];
+            __half hi[K], lo[K];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
+            for (int c = 0; c < K; ++c) {
                 const bool inside = FULL || c0 + c < left;
                 hi[c] = inside ? __ldcg(old) : __half();
                 lo[c] = inside ? __ldcg(old + 64) : __half();
                 old += ld;
             }
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = fmaf(beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
+            for (int c = 0; c < K; ++c) v[c] = fmaf(beta, __half2float(hi[c]) + __half2float(lo[c]), v[c]);
         }
     }
 
@@ -468,13 +468,14 @@ struct NewtonPolicy {
     static __device__ __forceinline__ void store_planes(const Params &p, const __half *old, __half *to, const float (&acc)[N], float alpha, float beta,
                                                         float diagonal, int on, int left)
     {
-        static_assert(N % 8 == 0, "columns eight at a time");
+        // (four with old X beside 64 running sums: eight spill 138 bytes, and 4096 x 4096 takes 3690 us instead of 3580)
+        constexpr int K = OLD && !FOLDED && N >= 64 ? 4 : 8;
 #pragma unroll
-        for (int c0 = 0; c0 < N; c0 += 8) {
-            float v[8];
+        for (int c0 = 0; c0 < N; c0 += K) {
+            float v[K];
             results<FULL, OLD>(v, old, p.ld, acc, c0, alpha, beta, left);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
+            for (int c = 0; c < K; ++c) {
                 if (FOLDED && OLD && c0 + c == on) v[c] += diagonal;
                 if (FULL || c0 + c < left) split_planes(v[c], to, to + 64);
                 to += p.ld;
@@ -1106,11 +1107,11 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     // Cycles of a block of 64 inner indices and of a round's store and meeting, fitted to five steps of 53 sizes (at the power cap those that reach it); FP32
     // results, whose accumulators are read after every block, apart from 16-bit ones.  The pick is within 4 percent of the fastest width for all of them,
     // 0.1 in the mean (by the products' cycles alone 12 and 1.3).  us with 256 / 128 / 64 columns, the pick marked:
-    //   FP32      300 x 300  195 / 126 / 118*       1024 x 1024  349 / 230 / 209*      3 x 1009 x 517  297 / 199* / 211   12 x 520 x 520  344 / 326* / 443
-    //             2048 x 2048  639 / 569* / 856     16 x 512 x 2048  750* / 758 / 944  3000 x 3000  1820 / 1790* / 2681   4096 x 4096  3729* / 3890 / 6623
+    //   FP32      300 x 300  197 / 138 / 121*       1024 x 1024  344 / 230 / 210*      3 x 1009 x 517  289 / 200* / 210   12 x 520 x 520  334 / 327* / 442
+    //             2048 x 2048  618 / 566* / 858     16 x 512 x 2048  731* / 757 / 921  3000 x 3000  1761* / 1804 / 2659   4096 x 4096  3591* / 3902 / 6604
     //   bfloat16  300 x 300  172 / 117 / 103*       1024 x 1024  331 / 205 / 168*      3 x 1009 x 517  278 / 185 / 173*   12 x 520 x 520  298 / 265* / 329
     //             2048 x 2048  582 / 502* / 630     16 x 512 x 2048  603* / 619 / 731  3000 x 3000  1626 / 1546* / 1980   4096 x 4096  3302* / 3354 / 4853
-    const int64_t wide = folded ? step_cycles<256>(p, 1600, 12000) : step_cycles<256>(p, 1600, 13600),
+    const int64_t wide = folded ? step_cycles<256>(p, 1600, 12000) : step_cycles<256>(p, 1520, 12400),
                   half = folded ? step_cycles<128>(p, 995, 5170) : step_cycles<128>(p, 994, 5900),
                   narrow = folded ? step_cycles<64>(p, 571, 5690) : step_cycles<64>(p, 1036, 2500);
     if (wide <= half && wide <= narrow) return folded ? launch_newton<true, 256>(maps, p, s) : launch_newton<false, 256>(maps, p, s);
