@@ -428,9 +428,10 @@ oz_status_t launch_tensor(GroupedParams p, oz_type_t type, bool *taken, cudaStre
     // 256 / 320 / 384 / 512, weight gradients 2048 x 4096 of 16 experts, 16384 tokens (such a product: 2.8e-7): 2.3e-7, 273 / 2.8e-7, 268 / 3.3e-7, 265 /
     // 4.4e-7, 265; input gradients of the same (3.9e-7): 2.4e-7, 237 / 2.9e-7, 230 / 3.4e-7, 229 / 4.7e-7, 225; forward, 8192 tokens, 8 experts 4096 x
     // 4096 (6.1e-7): 2.4e-7, 229 / 2.9e-7, 217 / 3.5e-7, 214 / 4.8e-7, 214.  (The epilogue adds up every segment, and, still storing the tile before,
-    // holds up the MMAs after two.)  Of 4096 for 16-bit results, which keeps what is cut off, 2^-24 of the sum 256 times in the mean, a tenth of a
-    // half-precision rounding.
-    p.core.seg = p.ctype == OZ_F32 ? 5 : 64;
+    // holds up the MMAs after two.)  Of 1024 for 16-bit results: 1.0e-6 before they are rounded, for a percent at most (512 / 1024 / 2048 / 4096: forward as
+    // above 4.9e-7, 235 / 1.0e-6, 229 / 2.1e-6, 226 / 4.4e-6, 226; the forward pass of 128 tokens 90.0 / 89.4 / 89.0 / 88.8; sums of positive numbers,
+    // which only lose, 2.2e-6 with 1024 and 1.4e-5 with 4096, in half precision, whose products are cut off one by one, 6.1e-6 and 2.6e-5).
+    p.core.seg = p.ctype == OZ_F32 ? 5 : 16;
     const TileShape shape = INNER ? TileShape{2, 256, 1} : tile_shape(p);
     GroupedMaps maps;
     const int64_t za = p.shared_a ? 1 : p.groups;

@@ -403,3 +403,18 @@ def test_same_call_same_bits():
             dw = [run_wgrad(x, dy, offsets, torch.zeros(groups, m, k, dtype=out, device="cuda")) for _ in range(3)]
             for r in (y, dx, dw):
                 assert torch.equal(r[0], r[1]) and torch.equal(r[0], r[2])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_16_bit_results_are_rounded_from_fp32_sums(dtype):
+    """Of results that are not the exact value correctly rounded there are at most 4 times as many as a product in FP32 has: how many there are goes with the
+    error before the rounding, of which 4 times that of FP32 is what the update of a parameter is held to as well."""
+    K = 4096
+    x, w = tensor(512, K, dtype=dtype, seed=46), tensor(1, 1024, K, dtype=dtype, seed=47, scale=1 / 64)
+    zero = torch.zeros(512, 1024, dtype=dtype, device="cuda")
+    y = run_grouped(x, w, offsets_of([512]), zero.clone(), 1)
+    dx = run_grouped(x, w.transpose(1, 2).contiguous(), offsets_of([512]), zero.clone(), 0)
+    grad = run_wgrad(w[0].T.contiguous(), x.T.contiguous(), offsets_of([K]), zero[None].clone())[0]
+    rounded, plain = (x.double() @ w[0].double().T).to(dtype), (x.float() @ w[0].float().T).to(dtype)
+    for got in (y, dx, grad):
+        assert (got != rounded).sum() <= 4 * (plain != rounded).sum()
