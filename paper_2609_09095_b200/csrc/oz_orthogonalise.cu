@@ -17,7 +17,7 @@
 //
 // Launches: sum of squares, planes of X, all products; narrow matrices: one.  Floor: (r r c + r r r + 2 r r c) operations a step and matrix,
 // three times that on the pipe.  Five steps: 4096 x 4096 in FP32 3.6 ms, 1.15 PFLOP/s on the pipe (power cap; the FP32 iteration of a library 34);
-// 16 x 512 x 2048 in bfloat16 600 us (gram on 48 of 74 pairs, 256 tiles of P X in 4 rounds); 1024 x 1024 168 us, 10 us a phase: 6.6 of them products, the rest
+// 16 x 512 x 2048 in bfloat16 600 us (gram on 48 of 74 pairs, 256 tiles of P X in 4 rounds); 1024 x 1024 172 us, 10 us a phase: 6.6 of them products, the rest
 // storing, meeting and the first copies.
 #include <algorithm>
 #include <atomic>
@@ -1095,10 +1095,12 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     p.otype = otype;
     p.transposed = mp.transposed;
     p.arrived = mp.arrived;
-    // Blocks of 64 an accumulator: error of the result (16 x 512 x 2048, 1024 x 1024) 0.8e-6 and 0.7e-6 with one, 1.4e-6 and 1.2e-6 with two, 5.6e-6
-    // and 3.8e-6 with eight, where a rounding to 16 bits is 1.7e-3 (bfloat16) or 2e-4; the FP32 iteration in one precision has 2e-6 to 5e-6.
-    // a X through P's diagonal is cut off with the sums (1024 x 1024, two blocks: 1.2e-6 -> 3.0e-6) but needs no second reading of X: 245 -> 191 us.
-    p.core.seg = otype == OZ_F32 ? 1 : 8;
+    // Blocks of 64 an accumulator.  FP32 results: error (16 x 512 x 2048, 1024 x 1024) 0.8e-6 and 0.7e-6 with one, 1.4e-6 and 1.2e-6 with two; the FP32
+    // iteration in one precision has 2e-6 to 5e-6.  16-bit results: a X through P's diagonal is cut off with the sums (1024 x 1024, two blocks: 1.2e-6 -> 2.9e-6
+    // before the rounding) but needs no second reading of X (245 -> 191 us when that was built).  Error before the rounding and us with one / two / four /
+    // eight blocks: 1024 x 1024 1.1e-6, 203 / 2.9e-6, 183 / 6.3e-6, 173 / 1.3e-5, 168; 16 x 512 x 2048 1.1e-6, 632 / 3.0e-6, 612 / 6.8e-6, 591 / 1.5e-5, 592;
+    // 2048 x 2048 1.3e-6, 558 / 3.2e-6, 494 / 7.1e-6, 494 / 1.4e-5, 494.  Four: no more than about three errors of the FP32 iteration.
+    p.core.seg = otype == OZ_F32 ? 1 : 4;
     p.core.idesc = idesc16(false, 2);
     p.core.status = mp.status;
     std::copy(alpha, alpha + 3 * steps, p.alpha);
@@ -1109,8 +1111,8 @@ oz_status_t oz_orthogonalise(int64_t m, int64_t n, int64_t count, oz_type_t type
     // 0.1 in the mean (by the products' cycles alone 12 and 1.3).  us with 256 / 128 / 64 columns, the pick marked:
     //   FP32      300 x 300  197 / 138 / 121*       1024 x 1024  344 / 230 / 210*      3 x 1009 x 517  289 / 200* / 210   12 x 520 x 520  334 / 327* / 442
     //             2048 x 2048  618 / 566* / 858     16 x 512 x 2048  731* / 757 / 921  3000 x 3000  1761* / 1804 / 2659   4096 x 4096  3591* / 3902 / 6604
-    //   bfloat16  300 x 300  172 / 117 / 103*       1024 x 1024  331 / 205 / 168*      3 x 1009 x 517  278 / 185 / 173*   12 x 520 x 520  298 / 265* / 329
-    //             2048 x 2048  582 / 502* / 630     16 x 512 x 2048  603* / 619 / 731  3000 x 3000  1626 / 1546* / 1980   4096 x 4096  3302* / 3354 / 4853
+    //   bfloat16  300 x 300  185 / 126 / 107*       1024 x 1024  330 / 204 / 172*      3 x 1009 x 517  278 / 183 / 175*   12 x 520 x 520  295 / 267* / 340
+    //             2048 x 2048  579 / 497* / 658     16 x 512 x 2048  597* / 612 / 713  3000 x 3000  1642 / 1540* / 2041   4096 x 4096  3310* / 3361 / 4910
     const int64_t wide = folded ? step_cycles<256>(p, 1600, 12000) : step_cycles<256>(p, 1520, 12400),
                   half = folded ? step_cycles<128>(p, 995, 5170) : step_cycles<128>(p, 994, 5900),
                   narrow = folded ? step_cycles<64>(p, 571, 5690) : step_cycles<64>(p, 1036, 2500);

@@ -453,3 +453,19 @@ def test_update_of_experts_gradients_close():
         assert not o[1].any()
         used = [0, 2, 3]
         hold_near(o[used], dw[used])
+
+
+@pytest.mark.parametrize("count,rows,cols", [(1, 1024, 1024), (3, 1009, 517), (16, 512, 2048), (1, 2048, 2048), (2, 300, 260), (2, 100, 700)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_16_bit_results_are_rounded_from_fp32_accuracy(count, rows, cols, dtype):
+    """Held to 4 errors of the FP32 iteration before the rounding as well: at most 4 times as many results as that has are not the exact update correctly rounded
+    (how many there are goes with the error before the rounding), and 6 standard deviations of such a count."""
+    g = tensor(count, rows, cols, seed=27, dtype=dtype)
+    got = update(g, dtype)
+    mine = usual = 0
+    for i in range(count):
+        x = normalised(g[i], 1e-7)
+        rounded = iterate(x, 5, USUAL).to(dtype)
+        mine += (got[i] != rounded).sum().item()
+        usual += (iterate(x.float(), 5, USUAL).to(dtype) != rounded).sum().item()
+    assert mine <= 4 * usual + 6 * (4 * usual + 1) ** 0.5, (mine, usual)
