@@ -249,9 +249,9 @@ oz_status_t launch_plain(const GroupedParams &p, cudaStream_t stream)
 }
 
 // ---------------------------------------------------------------- tensor cores
-// Bound, large products: the tensor cores at the power cap (8192 columns, 4 groups, 4096 x 4096: 179 us, 1540 TFLOP/s, the library's product of the same
-// operations 180; tensor pipe 86 % active, operands read from memory once); few columns a group: memory (32 groups, 128 columns, 2048 x 4096:
-// 90 us, 6.0 TB/s); results of short sums: the stores, five cycles a warp's store of a column (32 weight gradients 1536 x 1024 of 32 tokens: 38 us in
+// Bound, large products: the tensor cores at the power cap (8192 columns, 4 groups, 4096 x 4096: 192 us, 1430 TFLOP/s, where the library's product of the
+// same operations takes 207 in the same run, 178 and 180 in a cooler one; tensor pipe 86 % active, operands read from memory once); few columns a
+// group: memory (32 groups, 128 columns, 2048 x 4096: 90 us, 6.0 TB/s); results of short sums: the stores, five cycles a warp's store of a column (32 weight gradients 1536 x 1024 of 32 tokens: 38 us in
 // FP32; in 16 bits 31, with neighbouring lanes exchanging numbers for four-byte stores 37, by rows 25).
 // Rows of a tile are rows of C (features, whatever the group's size), its columns are those of a group (tokens) or of C_g: a group of
 // few tokens then takes an MMA of few columns, and consecutive lanes hold consecutive elements of the column-major result.

@@ -38,8 +38,8 @@ def test_reconstruction_variants_spill_little(tmp_path):
 
 def test_products_of_16_bit_matrices_do_not_spill(tmp_path):
     """The epilogue warps keep up to 64 running sums a thread beside old values and addresses in 96 registers (104 are to be had)."""
-    for unit, kernels in (("oz_grouped.cu", ("product16_kernel", "grouped_plain_kernel")), ("oz_orthogonalise.cu", ("product16_kernel", "newton_small_kernel"))):
-        for kernel in kernels:
-            spills = _spills(unit, kernel, tmp_path)
-            assert len(spills) >= 4
-            assert {name: n for name, n in spills.items() if n > 0} == {}
+    for unit, kernels in (("oz_grouped.cu", {"product16_kernel": 7, "grouped_plain_kernel": 4}), ("oz_orthogonalise.cu", {"product16_kernel": 6, "newton_small_kernel": 12})):
+        spills = _spills(unit, "kernel", tmp_path)
+        for kernel, variants in kernels.items():
+            assert sum(kernel in name for name in spills) >= variants, kernel
+        assert {name: n for name, n in spills.items() if n > 0} == {}
